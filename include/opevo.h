@@ -469,6 +469,58 @@ int opevo_compare_rows_f32(const float *c, const float *ref_rows, const int32_t 
 int opevo_compare_f32_static(const float *c, const float *ref, int64_t n, void *stream,
                              double *result);
 
+/* ---------------------------------------------------- expert layers: routing and 8-bit products
+ * A layer of experts sends each of T tokens to k of E experts, has every expert multiply its tokens by weights of its own, and adds the
+ * results up for each token with the router's weights:  opevo_route_dispatch (or _dispatch_i8)  ->  opevo_matmul_i8_grouped  ->
+ * opevo_route_combine.  opevo_quantize_rows_i8 and opevo_matmul_i8 are the same product without experts.
+ *
+ * All pointers but `bytes` are DEVICE pointers, aligned to their elements; matrices have contiguous rows, `ld_*` elements apart (at least
+ * their width), of any alignment and width (1 to 2^24).  `dtype` is an opevo_dtype.  Calls are asynchronous on `stream`, allocate nothing, may be captured in a HIP
+ * graph, and use the workspace until their work on the stream has finished.  Every output is written whole, and no output may overlap an input.  Results do not depend on
+ * the run: sums have a fixed order.
+ *
+ * Slot s = t * k + j (fewer than 2^31) holds expert[s] in [0, experts), or anything else for a slot that is not held here (its expert lives elsewhere, or it was
+ * dropped).  Rows: the slots in stable order of their experts, those not held left out; offsets[e] .. offsets[e + 1] are the rows of expert e,
+ * row_of_slot[s] the row of slot s or -1.  Buffers of rows have room for tokens * k of them; the rows from offsets[experts] on belong to no slot. */
+#define OPEVO_ROUTE_MAX_EXPERTS 1024
+#define OPEVO_ROUTE_MAX_SLOTS   64      /* k, the slots of a token */
+
+/* Bytes of workspace (4-byte aligned; may be 0) that a dispatch of this size takes.  Host only. */
+int opevo_route_workspace(int64_t tokens, int k, int experts, size_t *bytes);
+/* offsets[experts + 1], row_of_slot[tokens * k], rows[row_of_slot[s]] = x[s / k]; rows of no slot are filled with zeros.  tokens = 0 writes the
+ * offsets alone (the other pointers may be NULL).  The gradient of x is opevo_route_combine of the rows' gradient with weight = NULL. */
+int opevo_route_dispatch(const int32_t *expert, int64_t tokens, int k, int experts, const void *x, int64_t ld_x,
+                         int dtype, int64_t width, int32_t *offsets, int32_t *row_of_slot, void *rows, int64_t ld_rows,
+                         void *workspace, size_t workspace_bytes, void *stream);
+/* The same with the rows in 8 bits, as opevo_quantize_rows_i8 makes them of a token: q[row][width], scale[row] (0 for rows of no slot). */
+int opevo_route_dispatch_i8(const int32_t *expert, int64_t tokens, int k, int experts, const void *x, int64_t ld_x,
+                            int dtype, int64_t width, int32_t *offsets, int32_t *row_of_slot, int8_t *q, int64_t ld_q,
+                            float *scale, void *workspace, size_t workspace_bytes, void *stream);
+/* y[t] = sum over j of weight[t * k + j] * rows[row_of_slot[t * k + j]], in fp32 in the order of j, rounded once to dtype; weight = NULL: 1.  Slots
+ * without a row add nothing, whatever their weight: a token without any gets zeros. */
+int opevo_route_combine(const void *rows, int64_t ld_rows, int dtype, const float *weight, const int32_t *row_of_slot,
+                        int64_t tokens, int k, int64_t width, void *y, int64_t ld_y, void *stream);
+/* The gradients of the combine for dy: drows[row_of_slot[s]] = weight[s] * dy[s / k] (zeros in rows of no slot) and
+ * dweight[s] = sum over the row of dy[s / k] * rows[row_of_slot[s]], in fp32 (0 for slots without a row). */
+int opevo_route_combine_grad(const void *dy, int64_t ld_dy, const void *rows, int64_t ld_rows, int dtype, const float *weight,
+                             const int32_t *row_of_slot, const int32_t *offsets, int experts, int64_t tokens, int k, int64_t width,
+                             void *drows, int64_t ld_drows, float *dweight, void *stream);
+/* Rows to 8 bits: with a = the largest magnitude of a row, scale = a / 127 and q = 127 x / a rounded to the nearest integer, ties to even
+ * (for bf16 / fp16 the rounding of the exact quotient; for fp32 inputs that of a quotient right to 2^-24).  A row of zeros has q = 0 and
+ * scale = 0; a row that holds an infinity or a NaN has q = 0 and scale = NaN, so that what is computed from it is NaN. */
+int opevo_quantize_rows_i8(const void *x, int64_t ld_x, int dtype, int64_t rows, int64_t width, int8_t *q, int64_t ld_q,
+                           float *scale, void *stream);
+/* C[m, n] = (sum over k of A[m, k] * B[n, k]) * (scale_a[m] * scale_b[n]), the sum exact in 32-bit integers, then rounded to fp32, multiplied, and rounded to
+ * out_dtype.  A [M][K], B [N][K] (an output channel a row), C [M][N].  M at most 2^21, N 2^24, K from 1 to 2^17 - 1; M = 0 or N = 0 does nothing. */
+int opevo_matmul_i8(const int8_t *a, int64_t lda, const float *scale_a, const int8_t *b, int64_t ldb, const float *scale_b,
+                    void *c, int64_t ldc, int out_dtype, int64_t M, int64_t N, int64_t K, void *stream);
+/* The same for rows of experts: rows offsets[e] .. offsets[e + 1] of A times B[e] ([experts][N][K], its rows all ldb apart), scale_b [experts][N]; rows of C from
+ * offsets[experts] on are filled with zeros.  offsets ascend from 0, as a dispatch writes them; with offsets that do not, some of the `rows` rows
+ * of C are left as they are or hold another expert's product, but nothing outside them is read or written. */
+int opevo_matmul_i8_grouped(const int8_t *a, int64_t lda, const float *scale_a, const int8_t *b, int64_t ldb,
+                            const float *scale_b, const int32_t *offsets, int experts, void *c, int64_t ldc, int out_dtype,
+                            int64_t rows, int64_t N, int64_t K, void *stream);
+
 /* -------------------------------------------------------- whole tuning run (Alg. 1) */
 typedef struct {
     const void *a, *b;         /* DEVICE inputs                                                  */

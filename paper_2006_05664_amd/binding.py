@@ -25,6 +25,7 @@ OPEVO_E_HIPRTC, OPEVO_E_HIP, OPEVO_E_PARITY, OPEVO_E_TOO_LARGE, OPEVO_E_STATE = 
 OPEVO_FACTOR, OPEVO_PERMUTATION, OPEVO_DISCRETE, OPEVO_CATEGORICAL = 0, 1, 2, 3
 OPEVO_MATMUL, OPEVO_BMM, OPEVO_CONV2D, OPEVO_BMM_TA = 0, 1, 2, 3
 OPEVO_F32, OPEVO_BF16, OPEVO_F16 = 0, 1, 2
+OPEVO_ROUTE_MAX_EXPERTS, OPEVO_ROUTE_MAX_SLOTS = 1024, 64
 OPEVO_TILE2, OPEVO_TILE4, OPEVO_TILE4X, OPEVO_TILE4P, OPEVO_TILE4K, OPEVO_TILE4C, OPEVO_TILE4T, OPEVO_TILE4A, OPEVO_TILE4L = 0, 1, 2, 3, 4, 5, 6, 7, 8
 
 
@@ -138,6 +139,14 @@ _SIGNATURES = {
     "opevo_compare_f32": [_vp, _vp, C.c_int64, _vp, _f64p, _f64p],
     "opevo_compare_rows_f32": [_vp, _vp, _vp, C.c_int64, C.c_int64, _vp, _f64p, _f64p],
     "opevo_compare_f32_static": [_vp, _vp, C.c_int64, _vp, _vp],
+    "opevo_route_workspace": [C.c_int64, C.c_int, C.c_int, C.POINTER(C.c_size_t)],
+    "opevo_route_dispatch": [_vp, C.c_int64, C.c_int, C.c_int, _vp, C.c_int64, C.c_int, C.c_int64, _vp, _vp, _vp, C.c_int64, _vp, C.c_size_t, _vp],
+    "opevo_route_dispatch_i8": [_vp, C.c_int64, C.c_int, C.c_int, _vp, C.c_int64, C.c_int, C.c_int64, _vp, _vp, _vp, C.c_int64, _vp, _vp, C.c_size_t, _vp],
+    "opevo_route_combine": [_vp, C.c_int64, C.c_int, _vp, _vp, C.c_int64, C.c_int, C.c_int64, _vp, C.c_int64, _vp],
+    "opevo_route_combine_grad": [_vp, C.c_int64, _vp, C.c_int64, C.c_int, _vp, _vp, _vp, C.c_int, C.c_int64, C.c_int, C.c_int64, _vp, C.c_int64, _vp, _vp],
+    "opevo_quantize_rows_i8": [_vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int64, _vp, _vp],
+    "opevo_matmul_i8": [_vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_int64, _vp],
+    "opevo_matmul_i8_grouped": [_vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, C.c_int, _vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_int64, _vp],
     "opevo_tune": [_vp, C.c_int, C.POINTER(opevo_tune_args), _i32p, C.POINTER(opevo_tune_result)],
 }
 for _name, _argtypes in _SIGNATURES.items():
@@ -562,6 +571,48 @@ def opevo_compare_rows_f32(c: int, ref_rows: int, row_index: int, n_rows: int, r
     mx, fro = C.c_double(), C.c_double()
     _check(lib.opevo_compare_rows_f32(c, ref_rows, row_index, n_rows, row_len, stream, C.byref(mx), C.byref(fro)))
     return mx.value, fro.value
+
+
+# --------------------------------------------------- expert layers: routing, 8-bit products
+def opevo_route_workspace(tokens: int, k: int, experts: int) -> int:
+    v = C.c_size_t()
+    _check(lib.opevo_route_workspace(tokens, k, experts, C.byref(v)))
+    return v.value
+
+
+def opevo_route_dispatch(expert: int, tokens: int, k: int, experts: int, x: int, ld_x: int, dtype: int, width: int, offsets: int, row_of_slot: int,
+                         rows: int, ld_rows: int, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib.opevo_route_dispatch(expert, tokens, k, experts, x, ld_x, dtype, width, offsets, row_of_slot, rows, ld_rows, workspace, workspace_bytes, stream))
+
+
+def opevo_route_dispatch_i8(expert: int, tokens: int, k: int, experts: int, x: int, ld_x: int, dtype: int, width: int, offsets: int, row_of_slot: int,
+                            q: int, ld_q: int, scale: int, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib.opevo_route_dispatch_i8(expert, tokens, k, experts, x, ld_x, dtype, width, offsets, row_of_slot, q, ld_q, scale, workspace, workspace_bytes, stream))
+
+
+def opevo_route_combine(rows: int, ld_rows: int, dtype: int, weight: int, row_of_slot: int, tokens: int, k: int, width: int, y: int, ld_y: int,
+                        stream: int = 0) -> None:
+    _check(lib.opevo_route_combine(rows, ld_rows, dtype, weight, row_of_slot, tokens, k, width, y, ld_y, stream))
+
+
+def opevo_route_combine_grad(dy: int, ld_dy: int, rows: int, ld_rows: int, dtype: int, weight: int, row_of_slot: int, offsets: int, experts: int, tokens: int,
+                             k: int, width: int, drows: int, ld_drows: int, dweight: int, stream: int = 0) -> None:
+    _check(lib.opevo_route_combine_grad(dy, ld_dy, rows, ld_rows, dtype, weight, row_of_slot, offsets, experts, tokens, k, width, drows, ld_drows, dweight, stream))
+
+
+def opevo_quantize_rows_i8(x: int, ld_x: int, dtype: int, rows: int, width: int, q: int, ld_q: int, scale: int, stream: int = 0) -> None:
+    _check(lib.opevo_quantize_rows_i8(x, ld_x, dtype, rows, width, q, ld_q, scale, stream))
+
+
+def opevo_matmul_i8(a: int, lda: int, scale_a: int, b: int, ldb: int, scale_b: int, c: int, ldc: int, out_dtype: int, M: int, N: int, K: int,
+                    stream: int = 0) -> None:
+    _check(lib.opevo_matmul_i8(a, lda, scale_a, b, ldb, scale_b, c, ldc, out_dtype, M, N, K, stream))
+
+
+def opevo_matmul_i8_grouped(a: int, lda: int, scale_a: int, b: int, ldb: int, scale_b: int, offsets: int, experts: int, c: int, ldc: int, out_dtype: int,
+                            rows: int, N: int, K: int, stream: int = 0) -> None:
+    """rows: how many rows A and C have; which expert a row belongs to stands in offsets, on the device."""
+    _check(lib.opevo_matmul_i8_grouped(a, lda, scale_a, b, ldb, scale_b, offsets, experts, c, ldc, out_dtype, rows, N, K, stream))
 
 
 def opevo_tune(op, variant: int, a: int, b: int, c: int, ref: Optional[int] = None, stream: int = 0,
