@@ -76,92 +76,469 @@ __device__ __forceinline__ bool find_rows(const Product &p, int bm, long tile, R
     return false;
 }
 
+// Writes a wave's MI x NI atoms, rows r.first + m0 .. and columns col0 .. of C.  Atom (i, j): lane l holds columns 4 * (l / 16) .. + 3 of row l % 16 (the MFMA takes B's
+// rows as its first operand).  Stored like that, an instruction would touch 16 rows, 32 bytes of each, and the scales would be loaded under a mask for every atom
+// (8192 x 4096 x 1024: 77 us, 27 of them for each tile's epilogue); the 16 rows of an atom row go through a piece of LDS of the wave's own instead and leave as whole
+// lines, 16 bytes a lane.
+template <typename T, int NI> constexpr int kPatch = 16 * (NI * 16 * (int)sizeof(T) + 16);   // bytes of LDS a wave takes
+template <typename T, int MI, int NI>
+__device__ __forceinline__ void store_tile(const Product &p, const Rows &r, int m0, int col0, const i32x4 (&acc)[MI][NI], int8_t *patch)
+{
+    constexpr int PITCH = NI * 16 * (int)sizeof(T) + 16, CPR = NI * (int)sizeof(T), V = 16 / (int)sizeof(T);   // bytes, 16-byte chunks of a row, elements of a chunk
+    const int lane = threadIdx.x & 63, cols = p.n - col0;
+    const float *sbp = p.sb + (long)r.expert * p.n + col0;
+    float sb[NI][4], sa[MI];
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+        const int c = j * 16 + (lane >> 4) * 4;
+        if (!r.zero && c + 4 <= cols) __builtin_memcpy(sb[j], sbp + c, 16);
+        else
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sb[j][e] = !r.zero && c + e < cols ? sbp[c + e] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const long m = r.first + m0 + i * 16 + (lane & 15);
+        sa[i] = !r.zero && m < r.last ? p.sa[m] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            T v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = narrow<T>((float)acc[i][j][e] * (sa[i] * sb[j][e]));
+            __builtin_memcpy(__builtin_assume_aligned(patch + (lane & 15) * PITCH + (j * 16 + (lane >> 4) * 4) * sizeof(T), 4 * sizeof(T)), v, sizeof v);
+        }
+        __builtin_amdgcn_wave_barrier();
+        const long row0 = r.first + m0 + i * 16;
+#pragma unroll
+        for (int u = 0; u < (16 * CPR + 63) / 64; ++u) {
+            const int at = u * 64 + lane, row = at / CPR, c = at % CPR * V;
+            if ((16 * CPR) % 64 != 0 && row >= 16) continue;
+            if (row0 + row >= r.last || c >= cols) continue;
+            T *dst = (T *)p.c + (row0 + row) * p.ldc + col0 + c;
+            const i32x4 w = *(const i32x4 *)(patch + row * PITCH + at % CPR * 16);
+            if (c + V <= cols) __builtin_memcpy(dst, &w, 16);
+            else {
+                T part[V];
+                __builtin_memcpy(part, &w, 16);
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (c + e < cols) dst[e] = part[e];
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
 // Four neighbouring columns of C from `col` on, those that exist.
 template <typename T>
-__device__ __forceinline__ void store4(T *row, int col, int n, float a, float b, float c, float d)
+__device__ __forceinline__ void store4(T *row, int col, int n, const float (&c)[4])
 {
-    const T v[4] = {narrow<T>(a), narrow<T>(b), narrow<T>(c), narrow<T>(d)};
+    const T v[4] = {narrow<T>(c[0]), narrow<T>(c[1]), narrow<T>(c[2]), narrow<T>(c[3])};
     if (col + 4 <= n) __builtin_memcpy(row + col, v, sizeof v);
     else
         for (int i = 0; i < 4; ++i)
             if (col + i < n) row[col + i] = v[i];
 }
 
-// 16 bytes of a row of K values from k on, zeros past its end.
+// 16 bytes of a row of K values from k on, zeros past its end.  The piece that K ends in comes as the row's last 16 bytes, shifted.
 __device__ __forceinline__ i32x4 load_chunk(const int8_t *row, int k, int end)
 {
     i32x4 v = {0, 0, 0, 0};
     if (k + 16 <= end) __builtin_memcpy(&v, row + k, 16);
     else if (k < end) {
-        for (int i = 0; k + i < end; ++i) v[i >> 2] |= (int)(uint8_t)row[k + i] << (8 * (i & 3));
+        if (end >= 16) {
+            unsigned __int128 w;
+            __builtin_memcpy(&w, row + end - 16, 16);
+            w >>= 8 * (k + 16 - end);
+            __builtin_memcpy(&v, &w, 16);
+        } else {
+            for (int i = 0; k + i < end; ++i) v[i >> 2] |= (int)(uint8_t)row[k + i] << (8 * (i & 3));
+        }
     }
     return v;
 }
 
-// Any extents, any alignment.  A workgroup of four waves owns 64 x 64; slabs of 64 values go through registers into LDS, rows 16 bytes apart
-// from a multiple of the banks.  The MFMA takes B's rows as its first operand, so that a lane holds four neighbouring columns of one row of C.
-template <typename T>
-__global__ __launch_bounds__(256)
-void product_any(Product p)
+// ------------------------------------------------------------------ few rows
+// For few rows the weights are all there is to read, each once, and the time is that of one trip to memory.  No LDS and no barrier stands between: every wave loads
+// its fragments from global memory into registers, 256 values along K a step (four MFMA steps), the next step's while it multiplies.  The W waves of a
+// workgroup share a tile of MI x NI atoms and deal the steps among themselves; their sums meet in LDS.  Loads take any alignment.
+template <int MI, int NI, int W>
+__global__ __launch_bounds__(W * 64)
+void product_thin(Product p)
 {
-    constexpr int BM = 64, BN = 64, BK = 64, PITCH = BK + 16;
-    __shared__ __attribute__((aligned(16))) int8_t As[BM * PITCH], Bs[BN * PITCH];
+    __shared__ i32x4 sums[W][MI * NI][64];
+    Rows r;
+    if (!find_rows(p, MI * 16, blockIdx.y, &r)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n0 = blockIdx.x * NI * 16;
+    i32x4 acc[MI][NI] = {};
+    if (!r.zero) {
+        const int8_t *row[MI + NI];
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const long m = r.first + i * 16 + (lane & 15);
+            row[i] = p.a + (m < r.last ? m : r.last - 1) * p.lda;
+        }
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int n = n0 + j * 16 + (lane & 15);
+            row[MI + j] = p.b + ((long)r.expert * p.n + (n < p.n ? n : p.n - 1)) * p.ldb;
+        }
+        const int kl = (lane >> 4) * 16, steps = (p.k + 255) / 256;
+        i32x4 v[MI + NI][4], w[MI + NI][4];
+        auto load = [&](i32x4 (&to)[MI + NI][4], int step) {
+            const int k0 = step * 256 + kl;
+            if (step * 256 + 256 <= p.k) {
+#pragma unroll
+                for (int i = 0; i < MI + NI; ++i)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) __builtin_memcpy(&to[i][u], row[i] + k0 + u * 64, 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < MI + NI; ++i)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) to[i][u] = load_chunk(row[i], k0 + u * 64, p.k);
+            }
+        };
+        auto multiply = [&](const i32x4 (&of)[MI + NI][4]) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(of[MI + j][u], of[i][u], acc[i][j], 0, 0, 0);
+        };
+        int s = wave;
+        if (s < steps) load(v, s);
+        for (; s < steps; s += 2 * W) {
+            if (s + W < steps) load(w, s + W);
+            multiply(v);
+            if (s + W >= steps) break;
+            if (s + 2 * W < steps) load(v, s + 2 * W);
+            multiply(w);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) sums[wave][i * NI + j][lane] = acc[i][j];
+    __syncthreads();
+    for (int at = wave; at < MI * NI; at += W) {
+        i32x4 sum = sums[0][at][lane];
+#pragma unroll
+        for (int o = 1; o < W; ++o) sum += sums[o][at][lane];
+        const long m = r.first + at / NI * 16 + (lane & 15);
+        const int col = n0 + at % NI * 16 + (lane >> 4) * 4;
+        if (m >= r.last) continue;
+        const float *sb = p.sb + (long)r.expert * p.n + col;
+        const float sa = r.zero ? 0.f : p.sa[m];
+        float c[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = !r.zero && col + e < p.n ? (float)sum[e] * (sa * sb[e]) : 0.f;
+        if (p.out == OPEVO_F32) store4((float *)p.c + m * p.ldc, col, p.n, c);
+        else if (p.out == OPEVO_BF16) store4((__bf16 *)p.c + m * p.ldc, col, p.n, c);
+        else store4((_Float16 *)p.c + m * p.ldc, col, p.n, c);
+    }
+}
+
+// ------------------------------------------------------------------ tiles
+// Workgroup tile BM x BN, slabs of 128 values, WM x WN waves of MI x NI atoms of 16 x 16 x 64, KG groups of such waves that take every KG-th slab and add up
+// their sums in LDS at the end (for grids that leave a compute unit one workgroup, whose slabs are a chain of latencies).  The 16-byte chunk c of a row sits at chunk
+// position c ^ (row / 2 % 8) of its row of the slab: the 16 lanes of a turn of a fragment read then fall on 16 different groups of banks.
+// Rows past the end repeat the last one (their results are not stored); chunks past K are zeros.
+// DIRECT: every wave issues wave-wide loads of 16 bytes a lane whose destination is LDS, eight rows of a slab an instruction, the chunk each lane loads chosen by the
+// permutation; a ring of STAGES slabs keeps STAGES - 1 in flight.  For operands whose pointers, row lengths and K are multiples of 16.
+// Otherwise the slabs pass through registers, from where they start on any address: two stages in LDS, the slab after them on its way.
+template <bool DIRECT_, int BM_, int BN_, int WM_, int WN_, int STAGES_, int KG_ = 1>
+struct Shape {
+    static constexpr bool DIRECT = DIRECT_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, BK = 128;
+    static constexpr int KG = KG_, NW = WM * WN, NT = NW * 64 * KG, MI = BM / WM / 16, NI = BN / WN / 16;
+    static constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, PER = LA + LB, STAGE = (BM + BN) * BK;
+    static_assert(MI * WM * 16 == BM && NI * WN * 16 == BN && LA * 8 * NW == BM && LB * 8 * NW == BN && STAGES >= 2 && (DIRECT || STAGES == 2) && STAGE * STAGES * KG <= 160 * 1024 && NW * KG <= 16, "");
+};
+
+// lane i's 16 bytes from base + off to LDS at lds + 16 i; the kernel places every wait these loads need itself.  The base goes through a scalar copy: a
+// vector instruction that wrote it (a lane brought back into a scalar register) is followed by wait states only where the compiler sees a memory instruction.
+__device__ __forceinline__ void load_to_lds(const int8_t *base, unsigned off, unsigned lds)
+{
+    const int8_t *copy;
+    asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0" : "=&s"(copy) : "v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
+#define WAIT_LGKM_VMCNT(n) __builtin_amdgcn_s_waitcnt(((n) & 0xf) | (((n) >> 4) << 14) | (0x7 << 4))
+#define WAIT_LGKM() __builtin_amdgcn_s_waitcnt(0xf | (0x3 << 14) | (0x7 << 4))
+#define BARRIER() do { asm volatile("" ::: "memory"); __builtin_amdgcn_s_barrier(); asm volatile("" ::: "memory"); } while (0)
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ const int8_t *uniform(const int8_t *p)
+{
+    const unsigned long long v = (unsigned long long)p;
+    return (const int8_t *)(((unsigned long long)(unsigned)uniform((int)(v >> 32)) << 32) | (unsigned)uniform((int)v));
+}
+
+template <typename S>
+__global__ __launch_bounds__(S::NT)
+void product_tile(Product p)
+{
+    constexpr int BM = S::BM, BN = S::BN, BK = S::BK, MI = S::MI, NI = S::NI, LA = S::LA, LB = S::LB, PER = S::PER;
+    __shared__ __attribute__((aligned(1024))) int8_t whole[S::KG * S::STAGES * S::STAGE];
+    static_assert(S::NW * kPatch<float, NI> <= S::KG * S::STAGES * S::STAGE && (S::KG - 1) * S::NW * MI * NI * 1024 <= S::KG * S::STAGES * S::STAGE, "");
     Rows r;
     if (!find_rows(p, BM, blockIdx.y, &r)) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
+    const int tid = threadIdx.x, lane = tid & 63, all = uniform(tid >> 6), group = all / S::NW, wave = all % S::NW, wm = wave / S::WN, wn = wave % S::WN;
     const int n0 = blockIdx.x * BN;
-    i32x4 acc[2][2] = {};
+    int8_t *const ring = whole + group * (S::STAGES * S::STAGE);
+    i32x4 acc[MI][NI] = {};
     if (!r.zero) {
-        const int row = tid >> 2, kc = (tid & 3) * 16;
-        const long am = r.first + row < r.last ? r.first + row : r.last - 1;
-        const int bn = n0 + row < p.n ? n0 + row : p.n - 1;
-        const int8_t *arow = p.a + am * p.lda, *brow = p.b + ((long)r.expert * p.n + bn) * p.ldb;
-        for (int k0 = 0; k0 < p.k; k0 += BK) {
-            const i32x4 av = load_chunk(arow, k0 + kc, p.k), bv = load_chunk(brow, k0 + kc, p.k);
-            __syncthreads();
-            *(i32x4 *)(As + row * PITCH + kc) = av;
-            *(i32x4 *)(Bs + row * PITCH + kc) = bv;
-            __syncthreads();
-            i32x4 af[2], bf[2];
+        const unsigned ring_at = uniform((int)(unsigned)(unsigned long)(__attribute__((address_space(3))) int8_t *)ring);
+        // this wave's pieces of a slab: eight rows each, lane -> row lane / 8, chunk position lane % 8
+        const int rows = (int)(r.last - r.first), cols = p.n - n0;
+        unsigned off[PER];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                af[i] = *(const i32x4 *)(As + (wm * 32 + i * 16 + (lane & 15)) * PITCH + (lane >> 4) * 16);
-                bf[i] = *(const i32x4 *)(Bs + (wn * 32 + i * 16 + (lane & 15)) * PITCH + (lane >> 4) * 16);
+        for (int t = 0; t < PER; ++t) {
+            const bool is_a = t < LA;
+            const int row = (is_a ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, limit = is_a ? rows : cols;
+            const int chunk = (lane & 7) ^ (row >> 1 & 7);
+            off[t] = (unsigned)(row < limit ? row : limit - 1) * (unsigned)(is_a ? p.lda : p.ldb) + chunk * 16;
+        }
+        const int8_t *abase = uniform(p.a + r.first * p.lda), *bbase = uniform(p.b + ((long)r.expert * p.n + n0) * p.ldb);
+        const int whole_slabs = p.k / BK, slabs = (p.k + BK - 1) / BK;
+        const int steps = (slabs + S::KG - 1) / S::KG;      // of every group; a slab past the last one is zeros
+        // This wave's share of a slab into a stage; a slab that K ends in, or that lies past it, is filled up with zeros.
+        auto issue = [&](int step, int stage) {
+            const int slab = step * S::KG + group;
+            const int8_t *as = abase + (long)slab * BK, *bs = bbase + (long)slab * BK;
+            const unsigned at = ring_at + stage * S::STAGE, at_a = at + wave * LA * 1024, at_b = at + BM * BK + wave * LB * 1024;
+            if (slab < whole_slabs) {
+#pragma unroll
+                for (int t = 0; t < PER; ++t) load_to_lds(t < LA ? as : bs, off[t], t < LA ? at_a + t * 1024 : at_b + (t - LA) * 1024);
+            } else {
+#pragma unroll
+                for (int t = 0; t < PER; ++t) {
+                    const int row = (t < LA ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, chunk = (lane & 7) ^ (row >> 1 & 7);
+                    const unsigned to = t < LA ? at_a + t * 1024 : at_b + (t - LA) * 1024;
+                    if (slab * BK + chunk * 16 < p.k) load_to_lds(t < LA ? as : bs, off[t], to);
+                    else *(i32x4 *)(ring + (to - ring_at) + lane * 16) = i32x4{0, 0, 0, 0};
+                }
             }
+        };
+        // The same by way of registers: fetch starts the loads, put stores what they brought.
+        i32x4 hold[PER];
+        auto fetch = [&](int step) {
+            const int slab = step * S::KG + group;
+            if (slab < whole_slabs) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+                for (int t = 0; t < PER; ++t) __builtin_memcpy(&hold[t], (t < LA ? abase : bbase) + (long)slab * BK + off[t], 16);
+            } else {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bf[j], af[i], acc[i][j], 0, 0, 0);
+                for (int t = 0; t < PER; ++t) {
+                    const int row = (t < LA ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, chunk = (lane & 7) ^ (row >> 1 & 7);
+                    hold[t] = load_chunk((t < LA ? abase : bbase) + off[t] - chunk * 16, slab * BK + chunk * 16, p.k);
+                }
+            }
+        };
+        auto put = [&](int stage) {
+#pragma unroll
+            for (int t = 0; t < PER; ++t) *(i32x4 *)(ring + stage * S::STAGE + (t < LA ? (wave * LA + t) * 1024 : BM * BK + (wave * LB + t - LA) * 1024) + lane * 16) = hold[t];
+        };
+        // a stage that every wave has read is filled with the slab `step`
+        auto refill = [&](int step, int stage) {
+            if (S::DIRECT) issue(step, stage);
+            else {
+                put(stage);
+                if (step + 1 < steps) fetch(step + 1);
+            }
+        };
+        // this wave has read its part of a slab, and its part of the next one has landed
+        auto wait_next = [&](bool more) {
+            if (!S::DIRECT) WAIT_LGKM();
+            else if (S::STAGES > 2 && more) WAIT_LGKM_VMCNT((S::STAGES - 2) * PER);
+            else WAIT_LGKM_VMCNT(0);
+        };
+        // fragments: lane l holds row l % 16, the 16 values from 16 * (l / 16) of a step of 64
+        const int sw = lane >> 1 & 7, fr = lane & 15;
+        // prologue: slabs 0 .. STAGES - 1 under way, slab 0 landed, its first fragments read
+        if (!S::DIRECT) fetch(0);
+#pragma unroll
+        for (int s = 0; s < S::STAGES; ++s)
+            if (s < steps) refill(s, s);
+        if (!S::DIRECT) WAIT_LGKM();
+        else if (S::STAGES > 2 && steps > S::STAGES) WAIT_LGKM_VMCNT((S::STAGES - 1) * PER);
+        else WAIT_LGKM_VMCNT(0);
+        BARRIER();
+        if constexpr (MI * NI <= 4) {
+            // Few MFMAs a slab: reading a step's fragments takes longer than multiplying the step before.  The fragments of a whole slab are read at once, while the
+            // slab before it is multiplied.
+            i32x4 ag[2][2][MI], bg[2][2][NI];
+            auto read_slab = [&](int set, int stage) {
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    const int8_t *at = ring + stage * S::STAGE + (((kk * 4 + (lane >> 4)) ^ sw) << 4);
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) bg[set][kk][i] = *(const i32x4 *)(at + BM * BK + (wn * NI * 16 + i * 16 + fr) * BK);
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) ag[set][kk][i] = *(const i32x4 *)(at + (wm * MI * 16 + i * 16 + fr) * BK);
+                }
+            };
+            read_slab(0, 0);
+            int stage = 0;
+            auto slab = [&](int q, int set) {
+                const int next = stage + 1 == S::STAGES ? 0 : stage + 1;
+                const bool more = q + S::STAGES < steps;
+                wait_next(more);
+                BARRIER();                  // every wave has read slab q, and slab q + 1 has landed
+                read_slab(set ^ 1, next);
+                if (more) refill(q + S::STAGES, stage);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                    for (int m = 0; m < MI * NI; ++m)
+                        acc[m / NI][m % NI] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bg[set][kk][m % NI], ag[set][kk][m / NI], acc[m / NI][m % NI], 0, 0, 0);
+                stage = next;
+            };
+            int q = 0;
+            for (; q + 2 <= steps; q += 2) { slab(q, 0); slab(q + 1, 1); }
+            if (q < steps) slab(q, 0);
+        } else {
+        i32x4 af[2][MI], bf[2][NI];
+        auto read = [&](int buf, int stage, int kk, int i) {
+            const int8_t *at = ring + stage * S::STAGE + (((kk * 4 + (lane >> 4)) ^ sw) << 4);
+            if (i < NI) bf[buf][i] = *(const i32x4 *)(at + BM * BK + (wn * NI * 16 + i * 16 + fr) * BK);
+            else af[buf][i - NI] = *(const i32x4 *)(at + (wm * MI * 16 + (i - NI) * 16 + fr) * BK);
+        };
+#pragma unroll
+        for (int i = 0; i < MI + NI; ++i) read(0, 0, 0, i);
+        // A slab in two steps of 64.  Between the MFMAs of the first the wave reads the second's fragments; behind the first MFMA of the second step every wave has
+        // read the slab and the next one has landed: its first fragments are read and the stage is refilled.  (After the last slab the reads
+        // fetch what the ring holds; nothing uses it.)
+        int stage = 0;
+        for (int q = 0; q < steps; ++q) {
+            constexpr int SLOTS = MI * NI, NR = MI + NI;
+            const int next = stage + 1 == S::STAGES ? 0 : stage + 1;
+            const bool more = q + S::STAGES < steps;
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+                for (int m = 0; m < SLOTS; ++m) {
+                    acc[m / NI][m % NI] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bf[kk][m % NI], af[kk][m / NI], acc[m / NI][m % NI], 0, 0, 0);
+                    if (kk == 1 && m == 0) {
+                        wait_next(more);
+                        BARRIER();
+                        if (more) refill(q + S::STAGES, stage);
+                    }
+                    const int lo = m * NR / SLOTS, hi = (m + 1) * NR / SLOTS;
+#pragma unroll
+                    for (int u = 0; u < NR / SLOTS + 1; ++u)
+                        if (lo + u < hi) read(kk ^ 1, kk == 0 ? stage : next, kk ^ 1, lo + u);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            stage = next;
         }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const long m = r.first + wm * 32 + i * 16 + (lane & 15);
-        if (m >= r.last) continue;
-        const float sa = r.zero ? 0.f : p.sa[m];
-        T *row = (T *)p.c + m * p.ldc;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int col = n0 + wn * 32 + j * 16 + (lane >> 4) * 4;
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = !r.zero && col + e < p.n ? (float)acc[i][j][e] * (sa * p.sb[(long)r.expert * p.n + col + e]) : 0.f;
-            store4(row, col, p.n, v[0], v[1], v[2], v[3]);
         }
+        WAIT_LGKM_VMCNT(0);
     }
+    __syncthreads();
+    if (S::KG > 1) {                        // the groups' sums meet in LDS
+        i32x4 *const sums = (i32x4 *)whole;
+        if (group > 0)
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) sums[((((group - 1) * S::NW + wave) * MI + i) * NI + j) * 64 + lane] = acc[i][j];
+        __syncthreads();
+        if (group == 0)
+#pragma unroll
+            for (int g = 0; g < S::KG - 1; ++g)
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) acc[i][j] += sums[(((g * S::NW + wave) * MI + i) * NI + j) * 64 + lane];
+        __syncthreads();
+        if (group > 0) return;
+    }
+    int8_t *const patch = whole + wave * kPatch<float, NI>;
+    if (p.out == OPEVO_F32) store_tile<float>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch);
+    else if (p.out == OPEVO_BF16) store_tile<__bf16>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch);
+    else store_tile<_Float16>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch);
 }
 
 using opevo::fail;
 
-template <typename T>
-int run_product(const Product &p, hipStream_t stream)
+// How many tiles of bm rows there can be at most.  Grouped: each expert's last one is ragged, and so is that of the rows of none.
+int64_t row_tiles(const Product &p, int bm) { return p.offsets ? std::min<int64_t>(p.m, p.m / bm + p.experts + 1) : (p.m + bm - 1) / bm; }
+
+template <typename S>
+int run_tile(const Product &p, hipStream_t stream)
 {
-    // grouped: an expert's last tile is ragged, and so is that of the rows of none
-    const int64_t tiles = p.offsets ? std::min<int64_t>(p.m, p.m / 64 + p.experts + 1) : (p.m + 63) / 64;
-    hipLaunchKernelGGL(product_any<T>, dim3((unsigned)((p.n + 63) / 64), (unsigned)tiles), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL(product_tile<S>, dim3((unsigned)((p.n + S::BN - 1) / S::BN), (unsigned)row_tiles(p, S::BM)), dim3(S::NT), 0, stream, p);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? OPEVO_OK : opevo::hip_fail(e, "product launch");
+}
+
+template <int MI, int NI, int W>
+int run_thin(const Product &p, hipStream_t stream)
+{
+    constexpr int BM = MI * 16, BN = NI * 16;
+    hipLaunchKernelGGL((product_thin<MI, NI, W>), dim3((unsigned)((p.n + BN - 1) / BN), (unsigned)row_tiles(p, BM)), dim3(W * 64), 0, stream, p);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? OPEVO_OK : opevo::hip_fail(e, "product launch");
+}
+
+// A kernel and what it takes, in us: launch + max(steps * chain, load * (tile + steps * rate)), where steps is how many slabs (thin: steps of 256 values) a wave
+// goes through and load the workgroups for each of the 256 compute units, rounded up where one fills a unit.  The first term is a workgroup's chain of latencies,
+// the second what a compute unit gets through.  The constants were fitted to the times of every kernel at 350 (rows apart by multiples of 16) and 250 (others)
+// random sizes of 1 - 8192 rows, 64 - 8192 columns and K of 64 - 8192; the kernel chosen by them took 1.6 % and 2.7 % more than the best of all of them in the
+// geometric mean, at most 1.4 times as much.
+struct Kernel {
+    int (*run)(const Product &, hipStream_t);
+    int bm, bn, step, ways;             // tile, K of a step, waves or groups that share the steps
+    bool round_up, thin;
+    float launch, chain, tile, rate;
+};
+const Kernel kDirect[] = {
+    {run_tile<Shape<true, 256, 256, 2, 4, 2>>, 256, 256, 128, 1, true, false, 0.8f, 1.3f, 8.7f, 1.14f},
+    {run_tile<Shape<true, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, false, false, 2.85f, 1.03f, 2.05f, 0.58f},
+    {run_tile<Shape<true, 128, 128, 2, 4, 4>>, 128, 128, 128, 1, true, false, 0.f, 0.f, 4.85f, 0.466f},
+    {run_tile<Shape<true, 64, 64, 2, 4, 4>>, 64, 64, 128, 1, false, false, 2.89f, 0.294f, 0.466f, 0.296f},
+    {run_tile<Shape<true, 32, 64, 1, 4, 4, 2>>, 32, 64, 128, 2, false, false, 2.77f, 0.388f, 1.3f, 0.507f},
+    {run_tile<Shape<true, 32, 32, 2, 2, 6, 2>>, 32, 32, 128, 2, false, false, 2.45f, 0.252f, 0.654f, 0.352f},
+    {run_thin<1, 1, 4>, 16, 16, 256, 4, false, true, 2.29f, 0.585f, 0.f, 0.958f},
+};
+const Kernel kAny[] = {
+    {run_tile<Shape<false, 128, 256, 2, 4, 2>>, 128, 256, 128, 1, true, false, 0.f, 0.f, 7.04f, 1.45f},
+    {run_tile<Shape<false, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, false, false, 3.84f, 0.99f, 3.87f, 1.1f},
+    {run_tile<Shape<false, 64, 64, 2, 4, 2>>, 64, 64, 128, 1, false, false, 3.01f, 0.503f, 1.22f, 0.477f},
+    {run_tile<Shape<false, 32, 32, 2, 2, 2, 2>>, 32, 32, 128, 2, false, false, 2.72f, 0.422f, 0.472f, 0.418f},
+    {run_tile<Shape<false, 32, 32, 2, 2, 2, 4>>, 32, 32, 128, 4, false, false, 2.51f, 0.779f, 0.834f, 0.86f},
+    {run_thin<1, 1, 4>, 16, 16, 256, 4, false, true, 1.17f, 2.01f, 0.f, 2.19f},
+};
+constexpr int64_t kThinRows = 64;       // beyond, the 16 rows of a thin tile read the weights too often
+
+int run_product(const Product &p, hipStream_t stream)
+{
+    const auto whole = [](const void *at, long ld) { return reinterpret_cast<uintptr_t>(at) % 16 == 0 && ld % 16 == 0; };
+    const bool direct = p.k % 16 == 0 && whole(p.a, p.lda) && whole(p.b, p.ldb);
+    // a tile's rows are addressed by 32-bit offsets from its first
+    const bool near = p.lda <= (1 << 24) && p.ldb <= (1 << 24);
+    if (!near) return run_thin<1, 1, 4>(p, stream);
+    // grouped: as if the rows were dealt evenly, which the host cannot know
+    const int64_t parts = p.offsets ? std::min<int64_t>(p.experts, p.m) : 1, rows = (p.m + parts - 1) / parts;
+    const Kernel *best = nullptr;
+    float least = 0.f;
+    const auto consider = [&](const Kernel &k) {
+        if (k.thin && rows > kThinRows) return;
+        const int64_t groups = parts * ((rows + k.bm - 1) / k.bm) * ((p.n + k.bn - 1) / k.bn), slabs = (p.k + k.step - 1) / k.step;
+        const float steps = (float)((slabs + k.ways - 1) / k.ways), load = k.round_up ? (float)((groups + 255) / 256) : (float)groups / 256.f;
+        const float us = k.launch + std::max(steps * k.chain, load * (k.tile + steps * k.rate));
+        if (!best || us < least) { best = &k; least = us; }
+    };
+    if (direct) for (const Kernel &k : kDirect) consider(k);
+    else for (const Kernel &k : kAny) consider(k);
+    return best->run(p, stream);
 }
 
 int check_operand(const char *who, const char *name, const void *p, int64_t ld, int64_t width, size_t bytes)
@@ -184,7 +561,7 @@ int product(const char *who, Product &p, int64_t m, int64_t n, int64_t k, int ex
     if (int rc = check_operand(who, "scale_b", p.sb, 1, 1, 4)) return rc;
     p.m = m; p.n = (int)n; p.k = (int)k; p.experts = experts;
     const hipStream_t on = static_cast<hipStream_t>(stream);
-    return p.out == OPEVO_F32 ? run_product<float>(p, on) : p.out == OPEVO_BF16 ? run_product<__bf16>(p, on) : run_product<_Float16>(p, on);
+    return run_product(p, on);
 }
 
 }  // namespace

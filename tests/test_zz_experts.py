@@ -411,6 +411,25 @@ def test_rows_more_than_32_bits_apart():
 
 
 @gpu
+@pytest.mark.parametrize("ld", [1 << 24, (1 << 24) + 16, (1 << 24) - 1])
+def test_products_of_many_rows_far_apart(ld):
+    """Rows of a tile up to 2^32 bytes apart, and beyond that."""
+    torch, _ = _torch()
+    rng = np.random.default_rng(ld % 1000)
+    M, N, K = 300, 270, 160
+    av, bv = _eight(rng, M, K), _eight(rng, N, K)
+    far_a, far_b = (torch.empty(n * ld + K, dtype=torch.int8, device="cuda") for n in (M - 1, N - 1))
+    torch.as_strided(far_a, (M, K), (ld, 1)).copy_(torch.from_numpy(av))
+    torch.as_strided(far_b, (N, K), (ld, 1)).copy_(torch.from_numpy(bv))
+    near_b, ones, c = torch.from_numpy(bv).cuda(), torch.ones(M, device="cuda"), torch.empty(M, N, device="cuda")
+    want = torch.from_numpy(av.astype(np.float32) @ bv.astype(np.float32).T)
+    for b, ldb in ((far_b, ld), (near_b, K)):
+        c.fill_(float("nan"))
+        P.opevo_matmul_i8(far_a.data_ptr(), ld, ones.data_ptr(), b.data_ptr(), ldb, ones.data_ptr(), c.data_ptr(), N, P.OPEVO_F32, M, N, K)
+        assert torch.equal(c.cpu(), want)
+
+
+@gpu
 def test_offsets_that_no_dispatch_writes_touch_nothing_outside():
     rng = np.random.default_rng(11)
     rows, N, K, E = 20, 40, 48, 3
