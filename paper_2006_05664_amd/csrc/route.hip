@@ -17,24 +17,38 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxExperts = OPEVO_ROUTE_MAX_EXPERTS;
 
-template <typename T> struct Bits;
-template <> struct Bits<float> { typedef uint32_t type; };
-template <> struct Bits<_Float16> { typedef uint16_t type; };
-template <> struct Bits<__bf16> { typedef uint16_t type; };
-
-// 16 bytes of a row.  Rows start wherever the caller's row length puts them, so all such accesses are made for any alignment (the hardware's
-// 16-byte loads and stores take any address; the compiler is told nothing more).
+// A row is taken in pieces of 16 bytes.  Rows start wherever the caller's row length puts them, so all accesses are made for any alignment (the hardware's
+// 16-byte loads and stores take any address; the compiler is told nothing more).  Where the width is no multiple of a piece, the last piece ends with the row and overlaps the
+// one before it: both write the same values.  A row shorter than a piece is one, taken element by element.
 template <typename T> struct Vec {
     static constexpr int n = 16 / sizeof(T);
     T v[n];
 };
-template <typename T> __device__ __forceinline__ Vec<T> load16(const T *p)
-{
-    Vec<T> r;
-    __builtin_memcpy(&r, p, 16);
-    return r;
-}
-template <typename T> __device__ __forceinline__ void store16(T *p, const Vec<T> &r) { __builtin_memcpy(p, &r, 16); }
+template <typename T, bool WIDE> struct Pieces {     // WIDE: rows of at least a piece
+    int width, count;
+    __device__ explicit Pieces(int w) : width(w), count((w + Vec<T>::n - 1) / Vec<T>::n) {}
+    __device__ __forceinline__ int first(int i) const { return WIDE ? min(i * Vec<T>::n, width - Vec<T>::n) : 0; }
+    // how many of its elements the piece before has too
+    __device__ __forceinline__ int twice(int i) const { return WIDE ? i * Vec<T>::n - first(i) : 0; }
+    __device__ __forceinline__ Vec<T> load(const T *row, int i) const
+    {
+        Vec<T> r = {};
+        if (WIDE) __builtin_memcpy(&r, row + first(i), 16);
+        else
+#pragma unroll
+            for (int e = 0; e < Vec<T>::n; ++e)
+                if (e < width) r.v[e] = row[e];
+        return r;
+    }
+    template <typename O> __device__ __forceinline__ void store(O *row, int i, const O (&v)[Vec<T>::n]) const
+    {
+        if (WIDE) __builtin_memcpy(row + first(i), v, sizeof v);
+        else
+#pragma unroll
+            for (int e = 0; e < Vec<T>::n; ++e)
+                if (e < width) row[e] = v[e];
+    }
+};
 
 // ------------------------------------------------------------------ the sort
 // How many slots of a chunk go to each expert: counts[chunk][expert].
@@ -53,6 +67,8 @@ void route_count(const int *__restrict__ expert, long slots, int chunk, int expe
     for (int e = threadIdx.x; e < experts; e += kThreads) counts[(long)blockIdx.x * experts + e] = hist[e];
 }
 
+constexpr int kOwn = 64;                // slots of a workgroup at most: one wave ranks them
+
 struct Route {
     const int *expert;
     long tokens;
@@ -62,46 +78,52 @@ struct Route {
     int tokens_per_block;
     int *offsets, *row_of_slot;
 };
+struct Sorted { int total[kMaxExperts], before[kMaxExperts], place[kOwn], held; };
 
 // Rows of this workgroup's slots into place[] (-1: none), from the slots' experts alone: a slot's row is the number of slots of
 // lower experts, plus the earlier slots of its own.  Earlier slots are those of earlier chunks (counted by route_count, a column sum), those of
 // its chunk before this workgroup's first (counted here), and those of this workgroup before it.  Integer counts: any order gives the same.
-// Returns the number of slots that have a row.
-__device__ __forceinline__ int route_rows(const Route &r, long first_slot, int own, int *place, int *mine, int *total, int *before, bool writes)
+// held: the number of slots that have a row.
+__device__ __forceinline__ void route_rows(const Route &r, long first_slot, int own, Sorted &s, bool writes)
 {
-    const int tid = threadIdx.x;
-    const long slots = r.tokens * r.k;
-    for (int e = tid; e < r.experts; e += kThreads) total[e] = before[e] = 0;
-    if (tid < own) mine[tid] = r.expert[first_slot + tid];
+    const int tid = threadIdx.x, slot = tid < own ? r.expert[first_slot + tid] : -1;
+    for (int e = tid; e < r.experts; e += kThreads) s.total[e] = s.before[e] = 0;
     __syncthreads();
     if (r.counts) {
         const int at = (int)(first_slot / r.chunk);
-        for (int i = tid; i < r.chunks * r.experts; i += kThreads) {
-            const int n = r.counts[i], c = i / r.experts, e = i - c * r.experts;
-            if (n) {
-                atomicAdd(&total[e], n);
-                if (c < at) atomicAdd(&before[e], n);
+        const int lines = kThreads / r.experts > 1 ? kThreads / r.experts : 1, line = lines > 1 ? tid / r.experts : 0;
+        for (int e = lines > 1 ? tid - line * r.experts : tid; e < r.experts && line < lines; e += kThreads) {
+            int total = 0, before = 0;
+#pragma unroll 4
+            for (int c = line; c < r.chunks; c += lines) {
+                const int n = r.counts[c * r.experts + e];
+                total += n;
+                before += c < at ? n : 0;
             }
+            atomicAdd(&s.total[e], total);
+            atomicAdd(&s.before[e], before);
         }
-        for (long s = (long)at * r.chunk + tid; s < first_slot; s += kThreads) {
-            const unsigned e = r.expert[s];
-            if (e < (unsigned)r.experts) atomicAdd(&before[e], 1);
+        for (long i = (long)at * r.chunk + tid; i < first_slot; i += kThreads) {
+            const unsigned e = r.expert[i];
+            if (e < (unsigned)r.experts) atomicAdd(&s.before[e], 1);
         }
     } else {
-        for (long s = tid; s < slots; s += kThreads) {
-            const unsigned e = r.expert[s];
-            if (e < (unsigned)r.experts) {
-                atomicAdd(&total[e], 1);
-                if (s < first_slot) atomicAdd(&before[e], 1);
-            }
+        // both counts in one word, neither beyond 16 bits (kCountAlone slots at most)
+        const int slots = (int)(r.tokens * r.k);
+        for (int i0 = 0; i0 < slots; i0 += kThreads * 4) {
+            unsigned e[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) e[u] = i0 + u * kThreads + tid < slots ? (unsigned)r.expert[i0 + u * kThreads + tid] : ~0u;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (e[u] < (unsigned)r.experts) atomicAdd(&s.total[e[u]], i0 + u * kThreads + tid < first_slot ? 0x10001 : 1);
         }
     }
     __syncthreads();
-    __shared__ int held;
-    if (tid < 64) {                         // exclusive sums over the experts, 64 at a time
+    if (tid < 64) {                         // exclusive sums over the experts, 64 at a time, by the wave that has the slots
         int run = 0;
         for (int e0 = 0; e0 < r.experts; e0 += 64) {
-            const int e = e0 + tid, n = e < r.experts ? total[e] : 0;
+            const int e = e0 + tid, word = e < r.experts ? s.total[e] : 0, n = r.counts ? word : word & 0xffff;
             int sum = n;
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
@@ -109,115 +131,149 @@ __device__ __forceinline__ int route_rows(const Route &r, long first_slot, int o
                 if (tid >= o) sum += up;
             }
             if (e < r.experts) {
-                before[e] += run + sum - n;
+                s.before[e] = (r.counts ? s.before[e] : word >> 16) + run + sum - n;
                 if (writes) r.offsets[e] = run + sum - n;
             }
             run += __shfl(sum, 63);
         }
         if (tid == 0) {
-            held = run;
+            s.held = run;
             if (writes) r.offsets[r.experts] = run;
         }
-    }
-    __syncthreads();
-    if (tid < own) {
-        const int e = mine[tid];
-        int row = -1;
-        if ((unsigned)e < (unsigned)r.experts) {
-            row = before[e];
-            for (int i = 0; i < tid; ++i) row += mine[i] == e;
+        __builtin_amdgcn_wave_barrier();
+        int earlier = 0;
+        for (int i = 0; i < own; ++i) {
+            const int other = __builtin_amdgcn_readlane(slot, i);
+            earlier += i < tid && other == slot;
         }
-        place[tid] = row;
+        if (tid < own) s.place[tid] = (unsigned)slot < (unsigned)r.experts ? s.before[slot] + earlier : -1;
     }
     __syncthreads();
-    return held;
 }
 
-// Threads of a workgroup over rows of `vecs` pieces: `tx` lanes (a power of two) side by side on a row, the others on further rows.
-struct Lay { int tx, ty; };
-static Lay lay_out(int64_t vecs)
+struct Lay { int tx, ty, hold; };
+// `tx` lanes (a power of two) side by side on a row of `pieces`, `hold` pieces each, the others on further rows.  One piece a lane is the shortest way through a row; where there
+// are more rows than the chip holds at once, more pieces a lane keep more bytes on their way and leave a row to fewer waves.
+static Lay lay_out(int64_t pieces, int64_t rows, int most)
 {
-    int tx = 1;
-    while (tx < kThreads && tx < vecs) tx *= 2;
-    return {tx, kThreads / tx};
+    int tx = 1, hold = 1;
+    while (tx < kThreads && tx < pieces) tx *= 2;
+    while (hold < most && (tx * hold < pieces || (tx > 1 && rows * (tx / 2) / 64 >= 4096))) {
+        if (rows * (tx / 2) / 64 >= 4096 && tx * hold >= pieces) tx /= 2;
+        hold *= 2;
+    }
+    return {tx, kThreads / tx, hold};
 }
 
 // ------------------------------------------------------------------ dispatch
-template <typename T>
+// Bound by memory: 16384 tokens of 4096 bf16 to two rows each move 403 MB.  A token is read once and written k times; the first pieces are on their way while the slots
+// are sorted, the next ones while a piece is written.
+template <typename T, int kHold, bool WIDE>
 __global__ __launch_bounds__(kThreads)
 void route_dispatch(Route r, const T *__restrict__ x, long ld_x, int width, int tx, T *__restrict__ rows, long ld_rows)
 {
-    __shared__ int place[kThreads], mine[kThreads], total[kMaxExperts], before[kMaxExperts];
+    __shared__ Sorted s;
     const long first = (long)blockIdx.x * r.tokens_per_block;
     const int tokens = (int)(r.tokens - first < r.tokens_per_block ? r.tokens - first : r.tokens_per_block), own = tokens * r.k;
-    const int held = route_rows(r, first * r.k, own, place, mine, total, before, blockIdx.x == 0 && blockIdx.y == 0);
-    if (blockIdx.y == 0 && (int)threadIdx.x < own) r.row_of_slot[first * r.k + threadIdx.x] = place[threadIdx.x];
+    const Pieces<T, WIDE> at(width);
     const int lane = threadIdx.x % tx, ty = kThreads / tx, line = threadIdx.x / tx;
-    const int vecs = width / Vec<T>::n, step = tx * gridDim.y, start = blockIdx.y * tx + lane;
-    const int tail0 = vecs * Vec<T>::n;
-    for (int t = line; t < tokens; t += ty) {
-        const T *src = x + (first + t) * ld_x;
-        for (int c = start; c < vecs; c += step) {
-            const Vec<T> v = load16(src + c * Vec<T>::n);
-            for (int j = 0; j < r.k; ++j) {
-                const int row = place[t * r.k + j];
-                if (row >= 0) store16(rows + row * ld_rows + c * Vec<T>::n, v);
-            }
+    const int step = tx * gridDim.y * kHold, start = blockIdx.y * tx * kHold + lane;
+    Vec<T> v[kHold], w[kHold];
+    auto load = [&](Vec<T> (&to)[kHold], int t, int c) {
+#pragma unroll
+        for (int u = 0; u < kHold; ++u)
+            if (t < tokens && c + u * tx < at.count) to[u] = at.load(x + (first + t) * ld_x, c + u * tx);
+    };
+    int t = line, c = start;
+    load(v, t, c);
+    route_rows(r, first * r.k, own, s, blockIdx.x == 0 && blockIdx.y == 0);
+    if (blockIdx.y == 0 && (int)threadIdx.x < own) r.row_of_slot[first * r.k + threadIdx.x] = s.place[threadIdx.x];
+    while (t < tokens) {
+        int next_t = t, next_c = c + step;
+        if (next_c >= at.count) { next_t += ty; next_c = start; }
+        load(w, next_t, next_c);
+        for (int j = 0; j < r.k; ++j) {
+            const int row = s.place[t * r.k + j];
+            if (row < 0) continue;
+#pragma unroll
+            for (int u = 0; u < kHold; ++u)
+                if (c + u * tx < at.count) at.store(rows + row * ld_rows, c + u * tx, v[u].v);
         }
-        for (int c = tail0 + start; c < width; c += step) {
-            const T v = src[c];
-            for (int j = 0; j < r.k; ++j) {
-                const int row = place[t * r.k + j];
-                if (row >= 0) rows[row * ld_rows + c] = v;
-            }
-        }
+#pragma unroll
+        for (int u = 0; u < kHold; ++u) v[u] = w[u];
+        t = next_t; c = next_c;
     }
     // rows that no slot goes to
     const Vec<T> zero = {};
-    for (long row = held + (long)blockIdx.x * ty + line; row < r.tokens * r.k; row += (long)gridDim.x * ty) {
-        for (int c = start; c < vecs; c += step) store16(rows + row * ld_rows + c * Vec<T>::n, zero);
-        for (int c = tail0 + start; c < width; c += step) rows[row * ld_rows + c] = (T)0.f;
-    }
+    for (long row = s.held + (long)blockIdx.x * ty + line; row < r.tokens * r.k; row += (long)gridDim.x * ty)
+        for (int i = blockIdx.y * tx + lane; i < at.count; i += tx * gridDim.y) at.store(rows + row * ld_rows, i, zero.v);
 }
 
 // ------------------------------------------------------------------ rows to 8 bits
-// The largest magnitude as its bits: for numbers without a sign the order of the bits is that of the values, and infinities and
-// NaNs come last.
-constexpr unsigned kInfinite = 0x7f800000u;
-
-template <typename T> __device__ __forceinline__ unsigned magnitude(const Vec<T> &v)
+// Magnitudes as bits without the sign: their order is that of the values, and infinities and NaNs come last.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ unsigned magnitude(const Vec<float> &v)
 {
     unsigned m = 0;
 #pragma unroll
-    for (int i = 0; i < Vec<T>::n; ++i) m = max(m, __float_as_uint((float)v.v[i]) & 0x7fffffffu);
+    for (int i = 0; i < 4; ++i) m = max(m, __float_as_uint(v.v[i]) & 0x7fffffffu);
     return m;
 }
+template <typename T> __device__ __forceinline__ unsigned magnitude(const Vec<T> &v)
+{
+    unsigned w[4];
+    __builtin_memcpy(w, v.v, 16);
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+    return max(m.x, m.y);
+}
+template <typename T> __device__ __forceinline__ float value_of(unsigned m) { return (float)__builtin_bit_cast(T, (unsigned short)m); }
+template <> __device__ __forceinline__ float value_of<float>(unsigned m) { return __uint_as_float(m); }
 
 // q = round(127 x / a), a the row's largest magnitude.  With 127 x computed first (exact for 16-bit inputs: 11 + 7 bits) and one
 // division, the quotient of two numbers of at most 18 and 11 bits is a tie in fp32 only where it is one exactly, so the result is the
-// rounding of the exact quotient; fp32 inputs may differ from it where the quotient is within 2^-24 of a tie.
-struct Quantizer { float a, pre; bool finite; };
-__device__ __forceinline__ Quantizer quantizer(unsigned m)
-{
-    const float a = __uint_as_float(m);
-    const float pre = a > 1e30f ? 0.0078125f : 1.f;        // 127 x stays finite
-    return {a * pre, pre, m < kInfinite};
-}
-__device__ __forceinline__ int quantize(float x, const Quantizer &z)
-{
-    return z.finite && z.a > 0.f ? (int)rintf(127.f * (x * z.pre) / z.a) : 0;
-}
-__device__ __forceinline__ float scale_of(unsigned m)
-{
-    return m < kInfinite ? __uint_as_float(m) / 127.f : __uint_as_float(0x7fc00000u);
-}
-template <typename T> __device__ __forceinline__ void quantize16(const Vec<T> &v, const Quantizer &z, int8_t (&q)[Vec<T>::n])
-{
+// rounding of the exact quotient; fp32 inputs may differ from it where the quotient is within 2^-24 of a tie.  A division takes ten instructions: x times 127 / a, off by at most
+// 2e-5, rounds to the same integer unless it is within 1e-4 of a tie, and only then are the piece's eight values divided.
+template <typename T> struct Quantizer {
+    float a, pre, inv, scale;
+    bool on, plain;
+    __device__ explicit Quantizer(unsigned m)
+    {
+        const float largest = value_of<T>(m);
+        const bool finite = largest < __uint_as_float(0x7f800000u);
+        pre = largest > 1e30f ? 0x1p-7f : largest < 1e-30f ? 0x1p96f : 1.f;      // neither 127 x nor 127 / a overflows
+        a = largest * pre;
+        inv = 127.f / a;
+        on = finite && m > 0;
+        plain = pre == 1.f;
+        scale = finite ? largest / 127.f : __uint_as_float(0x7fc00000u);
+    }
+    __device__ __forceinline__ void operator()(const Vec<T> &x, int8_t (&q)[Vec<T>::n]) const
+    {
+        constexpr float kRound = 12582912.f;                // 1.5 * 2^23: what is added to it is rounded to an integer, in its low bits
+        unsigned word[Vec<T>::n];
+        float off = plain ? 0.f : 1.f;
 #pragma unroll
-    for (int i = 0; i < Vec<T>::n; ++i) q[i] = (int8_t)quantize((float)v.v[i], z);
-}
+        for (int i = 0; i < Vec<T>::n; ++i) {
+            const float y = (float)x.v[i] * inv, r = y + kRound;
+            off = fmaxf(off, fabsf(y - (r - kRound)));
+            word[i] = __float_as_uint(r);
+        }
+        if (off > 0.4999f)
+#pragma unroll
+            for (int i = 0; i < Vec<T>::n; ++i) word[i] = __float_as_uint(127.f * ((float)x.v[i] * pre) / a + kRound);
+        unsigned packed[Vec<T>::n / 4];
+#pragma unroll
+        for (int i = 0; i < Vec<T>::n / 4; ++i) {
+            const unsigned lo = __builtin_amdgcn_perm(word[4 * i + 1], word[4 * i], 0x0c0c0400u), hi = __builtin_amdgcn_perm(word[4 * i + 3], word[4 * i + 2], 0x04000c0cu);
+            packed[i] = on ? lo | hi : 0u;
+        }
+        __builtin_memcpy(q, packed, sizeof packed);
+    }
+};
 
-// The maximum over the tx lanes of a row (red: one word a wave).
+// The maximum over the tx lanes of a row (red: one word a wave).  tx > 64: for all threads of the workgroup together.
 __device__ __forceinline__ unsigned row_max(unsigned m, int tx, unsigned *red)
 {
     for (int o = 1; o < tx && o < 64; o <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, o));
@@ -231,86 +287,110 @@ __device__ __forceinline__ unsigned row_max(unsigned m, int tx, unsigned *red)
     return m;
 }
 
-template <typename T>
-__device__ __forceinline__ unsigned scan_row(const T *src, int width, int lane, int tx)
-{
-    const int vecs = width / Vec<T>::n;
-    unsigned m = 0;
-    for (int c = lane; c < vecs; c += tx) m = max(m, magnitude(load16(src + c * Vec<T>::n)));
-    for (int c = vecs * Vec<T>::n + lane; c < width; c += tx) m = max(m, __float_as_uint((float)src[c]) & 0x7fffffffu);
-    return m;
-}
+// A row's pieces in registers, as many as a lane holds; rows longer than that are read a second time for the pieces beyond.
+template <typename T, int HOLD, bool WIDE> struct Held {
+    Vec<T> v[HOLD];
+    unsigned m;
+    __device__ __forceinline__ void load(const Pieces<T, WIDE> &at, const T *row, int lane, int tx, bool on)
+    {
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u) {
+            v[u] = {};
+            if (on && lane + u * tx < at.count) v[u] = at.load(row, lane + u * tx);
+        }
+    }
+    __device__ __forceinline__ void scan(const Pieces<T, WIDE> &at, const T *row, int lane, int tx, bool on)
+    {
+        m = 0;
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u) m = max(m, magnitude(v[u]));
+        if (on)
+            for (int i = lane + HOLD * tx; i < at.count; i += tx) m = max(m, magnitude(at.load(row, i)));
+    }
+    template <typename F> __device__ __forceinline__ void each(const Pieces<T, WIDE> &at, const T *row, int lane, int tx, F &&f) const
+    {
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u)
+            if (lane + u * tx < at.count) f(lane + u * tx, v[u]);
+        for (int i = lane + HOLD * tx; i < at.count; i += tx) f(i, at.load(row, i));
+    }
+};
 
-template <typename T>
+template <typename T, int kHold, bool WIDE>
 __global__ __launch_bounds__(kThreads)
 void quantize_rows(const T *__restrict__ x, long ld_x, long rows, int width, int tx, int8_t *__restrict__ q, long ld_q, float *__restrict__ scale)
 {
     __shared__ unsigned red[kThreads / 64];
-    const int lane = threadIdx.x % tx, ty = kThreads / tx, vecs = width / Vec<T>::n;
+    const int lane = threadIdx.x % tx, ty = kThreads / tx;
     const long row = (long)blockIdx.x * ty + threadIdx.x / tx;
     const bool on = row < rows;
     const T *src = x + (on ? row : 0) * ld_x;
-    const unsigned m = row_max(on ? scan_row(src, width, lane, tx) : 0u, tx, red);
+    const Pieces<T, WIDE> at(width);
+    Held<T, kHold, WIDE> h;
+    h.load(at, src, lane, tx, on);
+    h.scan(at, src, lane, tx, on);
+    const unsigned m = row_max(h.m, tx, red);
     if (!on) return;
-    const Quantizer z = quantizer(m);
-    int8_t *dst = q + row * ld_q;
-    for (int c = lane; c < vecs; c += tx) {
+    const Quantizer<T> z(m);
+    h.each(at, src, lane, tx, [&](int i, const Vec<T> &v) {
         int8_t out[Vec<T>::n];
-        quantize16(load16(src + c * Vec<T>::n), z, out);
-        __builtin_memcpy(dst + c * Vec<T>::n, out, sizeof out);
-    }
-    for (int c = vecs * Vec<T>::n + lane; c < width; c += tx) dst[c] = (int8_t)quantize((float)src[c], z);
-    if (lane == 0) scale[row] = scale_of(m);
+        z(v, out);
+        at.store(q + row * ld_q, i, out);
+    });
+    if (lane == 0) scale[row] = z.scale;
 }
 
-template <typename T>
+template <typename T, int kHold, bool WIDE>
 __global__ __launch_bounds__(kThreads)
 void route_dispatch_i8(Route r, const T *__restrict__ x, long ld_x, int width, int tx, int8_t *__restrict__ q, long ld_q, float *__restrict__ scale)
 {
-    __shared__ int place[kThreads], mine[kThreads], total[kMaxExperts], before[kMaxExperts];
+    __shared__ Sorted s;
     __shared__ unsigned red[kThreads / 64];
     const long first = (long)blockIdx.x * r.tokens_per_block;
     const int tokens = (int)(r.tokens - first < r.tokens_per_block ? r.tokens - first : r.tokens_per_block), own = tokens * r.k;
-    const int held = route_rows(r, first * r.k, own, place, mine, total, before, blockIdx.x == 0);
-    if ((int)threadIdx.x < own) r.row_of_slot[first * r.k + threadIdx.x] = place[threadIdx.x];
     const int lane = threadIdx.x % tx, ty = kThreads / tx, line = threadIdx.x / tx;
-    const int vecs = width / Vec<T>::n;
-    for (int t0 = 0; t0 < tokens; t0 += ty) {
+    const Pieces<T, WIDE> at(width);
+    Held<T, kHold, WIDE> h, next;
+    h.load(at, x + (first + line) * ld_x, lane, tx, line < tokens);
+    route_rows(r, first * r.k, own, s, blockIdx.x == 0);
+    if ((int)threadIdx.x < own) r.row_of_slot[first * r.k + threadIdx.x] = s.place[threadIdx.x];
+    for (int t0 = 0; t0 < tokens; t0 += ty) {               // alike for all threads: row_max is for all together
         const int t = t0 + line;
         const bool on = t < tokens;
-        const T *src = x + (first + (on ? t : 0)) * ld_x;
-        const unsigned m = row_max(on ? scan_row(src, width, lane, tx) : 0u, tx, red);
-        if (!on) continue;                  // every lane of a row's line alike; a line longer than a wave is the whole workgroup's trip
-        const Quantizer z = quantizer(m);
-        for (int c = lane; c < vecs; c += tx) {
-            int8_t out[Vec<T>::n];
-            quantize16(load16(src + c * Vec<T>::n), z, out);
-            for (int j = 0; j < r.k; ++j) {
-                const int row = place[t * r.k + j];
-                if (row >= 0) __builtin_memcpy(q + row * ld_q + c * Vec<T>::n, out, sizeof out);
+        const T *src = x + (first + t) * ld_x;
+        next.load(at, src + ty * ld_x, lane, tx, t + ty < tokens);
+        h.scan(at, src, lane, tx, on);
+        const unsigned m = row_max(h.m, tx, red);
+        if (on) {
+            const Quantizer<T> z(m);
+            h.each(at, src, lane, tx, [&](int i, const Vec<T> &v) {
+                int8_t out[Vec<T>::n];
+                z(v, out);
+                for (int j = 0; j < r.k; ++j) {
+                    const int row = s.place[t * r.k + j];
+                    if (row >= 0) at.store(q + row * ld_q, i, out);
+                }
+            });
+            for (int j = lane; j < r.k; j += tx) {
+                const int row = s.place[t * r.k + j];
+                if (row >= 0) scale[row] = z.scale;
             }
         }
-        for (int c = vecs * Vec<T>::n + lane; c < width; c += tx) {
-            const int8_t out = (int8_t)quantize((float)src[c], z);
-            for (int j = 0; j < r.k; ++j) {
-                const int row = place[t * r.k + j];
-                if (row >= 0) q[row * ld_q + c] = out;
-            }
-        }
-        for (int j = lane; j < r.k; j += tx) {
-            const int row = place[t * r.k + j];
-            if (row >= 0) scale[row] = scale_of(m);
-        }
+        h = next;
     }
-    for (long row = held + (long)blockIdx.x * ty + line; row < r.tokens * r.k; row += (long)gridDim.x * ty) {
-        for (int c = lane; c < width; c += tx) q[row * ld_q + c] = 0;
+    const int8_t zero[Vec<T>::n] = {};
+    for (long row = s.held + (long)blockIdx.x * ty + line; row < r.tokens * r.k; row += (long)gridDim.x * ty) {
+        for (int i = lane; i < at.count; i += tx) at.store(q + row * ld_q, i, zero);
         if (lane == 0) scale[row] = 0.f;
     }
 }
 
 // ------------------------------------------------------------------ combine
-// y[t] = sum_j w[t, j] rows[row_of_slot[t, j]], j ascending, in fp32, rounded once; a slot without a row adds nothing, whatever its weight.
-template <typename T>
+// y[t] = sum_j w[t, j] rows[row_of_slot[t, j]], j ascending, in fp32, rounded once; a slot without a row adds nothing, whatever its weight.  Bound by memory: the rows
+// of J slots are on their way together.
+constexpr int kSlots = 4;               // J
+
+template <typename T, bool WIDE>
 __global__ __launch_bounds__(kThreads)
 void route_combine(const T *__restrict__ rows, long ld_rows, const float *__restrict__ weight, const int *__restrict__ row_of_slot,
                    long tokens, int k, int width, int tx, T *__restrict__ y, long ld_y)
@@ -318,84 +398,86 @@ void route_combine(const T *__restrict__ rows, long ld_rows, const float *__rest
     const int lane = threadIdx.x % tx, ty = kThreads / tx;
     const long t = (long)blockIdx.x * ty + threadIdx.x / tx, slots = tokens * k;
     if (t >= tokens) return;
-    const int vecs = width / Vec<T>::n, step = tx * gridDim.y, start = blockIdx.y * tx + lane;
-    for (int c = start; c < vecs; c += step) {
+    const Pieces<T, WIDE> at(width);
+    for (int i = blockIdx.y * tx + lane; i < at.count; i += tx * gridDim.y) {
         float sum[Vec<T>::n] = {};
-        for (int j = 0; j < k; ++j) {
-            const int row = row_of_slot[t * k + j];
-            if ((unsigned)row >= (unsigned long)slots) continue;
-            const float w = weight ? weight[t * k + j] : 1.f;
-            const Vec<T> v = load16(rows + row * ld_rows + c * Vec<T>::n);
+        for (int j0 = 0; j0 < k; j0 += kSlots) {
+            Vec<T> v[kSlots];
+            float w[kSlots];
+            bool has[kSlots];
 #pragma unroll
-            for (int i = 0; i < Vec<T>::n; ++i) sum[i] = fmaf(w, (float)v.v[i], sum[i]);
+            for (int j = 0; j < kSlots; ++j) {
+                const int row = j0 + j < k ? row_of_slot[t * k + j0 + j] : -1;
+                has[j] = (unsigned)row < (unsigned long)slots;
+                w[j] = weight && j0 + j < k ? weight[t * k + j0 + j] : 1.f;
+                if (has[j]) v[j] = at.load(rows + row * ld_rows, i);
+            }
+#pragma unroll
+            for (int j = 0; j < kSlots; ++j)
+                if (has[j])
+#pragma unroll
+                    for (int e = 0; e < Vec<T>::n; ++e) sum[e] = fmaf(w[j], (float)v[j].v[e], sum[e]);
         }
         Vec<T> out;
 #pragma unroll
-        for (int i = 0; i < Vec<T>::n; ++i) out.v[i] = narrow<T>(sum[i]);
-        store16(y + t * ld_y + c * Vec<T>::n, out);
-    }
-    for (int c = vecs * Vec<T>::n + start; c < width; c += step) {
-        float sum = 0.f;
-        for (int j = 0; j < k; ++j) {
-            const int row = row_of_slot[t * k + j];
-            if ((unsigned)row >= (unsigned long)slots) continue;
-            sum = fmaf(weight ? weight[t * k + j] : 1.f, (float)rows[row * ld_rows + c], sum);
-        }
-        y[t * ld_y + c] = narrow<T>(sum);
+        for (int e = 0; e < Vec<T>::n; ++e) out.v[e] = narrow<T>(sum[e]);
+        at.store(y + t * ld_y, i, out.v);
     }
 }
 
 // drows[row_of_slot[s]] = w[s] dy[s / k], dw[s] = <dy[s / k], rows[row_of_slot[s]]>; rows from offsets[experts] on get zeros, slots without a row dw = 0.
-template <typename T>
+// Bound by memory: 8192 tokens of 4096 bf16 with four rows each move 604 MB.  One row is read and one written at a time by as many waves as fit: dy, which each slot reads
+// again, comes from the caches.  (All slots' rows at once, dy's pieces and the next row's held in registers: 140 - 180 us instead of 127 for that size.)
+template <typename T, bool WIDE>
 __global__ __launch_bounds__(kThreads)
 void route_combine_grad(const T *__restrict__ dy, long ld_dy, const T *__restrict__ rows, long ld_rows, const float *__restrict__ weight,
                         const int *__restrict__ row_of_slot, const int *__restrict__ held_at, long tokens, int k, int width, int tx,
                         T *__restrict__ drows, long ld_drows, float *__restrict__ dweight)
 {
-    __shared__ float red[kThreads / 64];
+    __shared__ float red[OPEVO_ROUTE_MAX_SLOTS][kThreads / 64];
     const int lane = threadIdx.x % tx, ty = kThreads / tx, line = threadIdx.x / tx;
     const long t = (long)blockIdx.x * ty + line, slots = tokens * k;
     const bool on = t < tokens;
-    const int vecs = width / Vec<T>::n;
+    const Pieces<T, WIDE> at(width);
     for (int j = 0; j < k; ++j) {
         const int row = on ? row_of_slot[t * k + j] : -1;
-        const bool has = (unsigned)row < (unsigned long)slots;
-        const float w = has ? weight[t * k + j] : 0.f;
         float dot = 0.f;
-        if (has) {
-            for (int c = lane; c < vecs; c += tx) {
-                const Vec<T> g = load16(dy + t * ld_dy + c * Vec<T>::n), v = load16(rows + row * ld_rows + c * Vec<T>::n);
+        if ((unsigned)row < (unsigned long)slots) {
+            const float w = weight[t * k + j];
+            for (int i = lane; i < at.count; i += tx) {
+                const Vec<T> g = at.load(dy + t * ld_dy, i), v = at.load(rows + row * ld_rows, i);
+                const int twice = at.twice(i);
+                if (twice == 0)
+#pragma unroll
+                    for (int e = 0; e < Vec<T>::n; ++e) dot = fmaf((float)g.v[e], (float)v.v[e], dot);
+                else
+                    for (int e = 0; e < Vec<T>::n; ++e)
+                        if (e >= twice) dot = fmaf((float)g.v[e], (float)v.v[e], dot);
                 Vec<T> out;
 #pragma unroll
-                for (int i = 0; i < Vec<T>::n; ++i) {
-                    dot = fmaf((float)g.v[i], (float)v.v[i], dot);
-                    out.v[i] = narrow<T>(w * (float)g.v[i]);
-                }
-                store16(drows + row * ld_drows + c * Vec<T>::n, out);
-            }
-            for (int c = vecs * Vec<T>::n + lane; c < width; c += tx) {
-                const float g = (float)dy[t * ld_dy + c];
-                dot = fmaf(g, (float)rows[row * ld_rows + c], dot);
-                drows[row * ld_drows + c] = narrow<T>(w * g);
+                for (int e = 0; e < Vec<T>::n; ++e) out.v[e] = narrow<T>(w * (float)g.v[e]);
+                at.store(drows + row * ld_drows, i, out.v);
             }
         }
         for (int o = 1; o < tx && o < 64; o <<= 1) dot += __shfl_xor(dot, o);
-        if (tx > 64) {
-            __syncthreads();
-            if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = dot;
-            __syncthreads();
-            const int w0 = line * (tx / 64);
-            dot = 0.f;
-            for (int i = 0; i < tx / 64; ++i) dot += red[w0 + i];
+        if (tx <= 64) {
+            if (on && lane == 0) dweight[t * k + j] = dot;
+        } else if ((threadIdx.x & 63) == 0) {
+            red[j][threadIdx.x >> 6] = dot;
         }
-        if (on && lane == 0) dweight[t * k + j] = dot;
+    }
+    if (tx > 64) {
+        __syncthreads();
+        for (int j = lane; on && j < k; j += tx) {
+            float dot = 0.f;
+            for (int i = 0; i < tx / 64; ++i) dot += red[j][line * (tx / 64) + i];
+            dweight[t * k + j] = dot;
+        }
     }
     const Vec<T> zero = {};
     const int held = *held_at;
-    for (long row = (held > 0 ? held : 0) + (long)blockIdx.x * ty + line; row < slots; row += (long)gridDim.x * ty) {
-        for (int c = lane; c < vecs; c += tx) store16(drows + row * ld_drows + c * Vec<T>::n, zero);
-        for (int c = vecs * Vec<T>::n + lane; c < width; c += tx) drows[row * ld_drows + c] = (T)0.f;
-    }
+    for (long row = (held > 0 ? held : 0) + (long)blockIdx.x * ty + line; row < slots; row += (long)gridDim.x * ty)
+        for (int i = lane; i < at.count; i += tx) at.store(drows + row * ld_drows, i, zero.v);
 }
 
 // ------------------------------------------------------------------ host side
@@ -438,7 +520,7 @@ constexpr int64_t kCountAlone = 4096;
 int64_t chunk_of(int64_t slots, int experts)
 {
     int64_t chunk = 256;
-    while (chunk < 8192 && chunk * chunk < 2 * slots * experts) chunk *= 2;
+    while (chunk < 8192 && 2 * chunk * chunk < slots * experts) chunk *= 2;
     return chunk;
 }
 
@@ -460,37 +542,47 @@ int plan_route(const char *who, const int32_t *expert, int64_t tokens, int k, in
         if (int rc = launched("route_count launch")) return rc;
         r->counts = static_cast<const int *>(workspace);
     }
-    // as many tokens a workgroup as leave 1024 workgroups, and as have a slot for each thread
-    r->tokens_per_block = (int)std::max<int64_t>(1, std::min<int64_t>(kThreads / k, tokens / 1024));
     return OPEVO_OK;
 }
 
-template <typename T>
-int run_dispatch(const Route &r, const void *x, int64_t ld_x, int64_t width, void *rows, int64_t ld_rows, hipStream_t stream)
+// As many tokens a workgroup as leave 1024 workgroups, or one for each compute unit where every one counts all slots, in whole rounds of `ty`, but no more slots than a wave ranks.
+void deal(Route *r, int ty)
 {
-    const int64_t vecs = (width + Vec<T>::n - 1) / Vec<T>::n;
-    const Lay l = lay_out(vecs);
+    const int64_t most = kOwn / r->k, share = r->tokens / (r->counts ? 1024 : 256);
+    r->tokens_per_block = (int)std::max<int64_t>(1, std::min(std::max<int64_t>(ty, share / ty * ty), most));
+}
+
+template <typename T>
+int run_dispatch(Route r, const void *x, int64_t ld_x, int64_t width, void *rows, int64_t ld_rows, hipStream_t stream)
+{
+    const int64_t pieces = (width + Vec<T>::n - 1) / Vec<T>::n;
+    const Lay l = lay_out(pieces, r.tokens, 4);
+    deal(&r, l.ty);
     const int64_t blocks = std::max<int64_t>(1, (r.tokens + r.tokens_per_block - 1) / r.tokens_per_block);
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((vecs + l.tx - 1) / l.tx, 512 / blocks));
-    hipLaunchKernelGGL(route_dispatch<T>, dim3((unsigned)blocks, (unsigned)parts), dim3(kThreads), 0, stream, r, static_cast<const T *>(x), (long)ld_x,
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((pieces + l.tx * l.hold - 1) / (l.tx * l.hold), 512 / blocks));
+    auto *k = width < Vec<T>::n ? route_dispatch<T, 1, false> : l.hold == 1 ? route_dispatch<T, 1, true> : l.hold == 2 ? route_dispatch<T, 2, true> : route_dispatch<T, 4, true>;
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks, (unsigned)parts), dim3(kThreads), 0, stream, r, static_cast<const T *>(x), (long)ld_x,
                        (int)width, l.tx, static_cast<T *>(rows), (long)ld_rows);
     return launched("route_dispatch launch");
 }
 template <typename T>
-int run_dispatch_i8(const Route &r, const void *x, int64_t ld_x, int64_t width, int8_t *q, int64_t ld_q, float *scale, hipStream_t stream)
+int run_dispatch_i8(Route r, const void *x, int64_t ld_x, int64_t width, int8_t *q, int64_t ld_q, float *scale, hipStream_t stream)
 {
-    const Lay l = lay_out((width + Vec<T>::n - 1) / Vec<T>::n);
+    const Lay l = lay_out((width + Vec<T>::n - 1) / Vec<T>::n, r.tokens, 4);
+    deal(&r, l.ty);
     const int64_t blocks = std::max<int64_t>(1, (r.tokens + r.tokens_per_block - 1) / r.tokens_per_block);
-    hipLaunchKernelGGL(route_dispatch_i8<T>, dim3((unsigned)blocks), dim3(kThreads), 0, stream, r, static_cast<const T *>(x), (long)ld_x, (int)width, l.tx,
+    auto *k = width < Vec<T>::n ? route_dispatch_i8<T, 1, false> : l.hold == 1 ? route_dispatch_i8<T, 1, true> : l.hold == 2 ? route_dispatch_i8<T, 2, true> : route_dispatch_i8<T, 4, true>;
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kThreads), 0, stream, r, static_cast<const T *>(x), (long)ld_x, (int)width, l.tx,
                        q, (long)ld_q, scale);
     return launched("route_dispatch_i8 launch");
 }
 template <typename T>
 int run_quantize(const void *x, int64_t ld_x, int64_t rows, int64_t width, int8_t *q, int64_t ld_q, float *scale, hipStream_t stream)
 {
-    const Lay l = lay_out((width + Vec<T>::n - 1) / Vec<T>::n);
+    const Lay l = lay_out((width + Vec<T>::n - 1) / Vec<T>::n, rows, 4);
     const int64_t blocks = (rows + l.ty - 1) / l.ty;
-    hipLaunchKernelGGL(quantize_rows<T>, dim3((unsigned)blocks), dim3(kThreads), 0, stream, static_cast<const T *>(x), (long)ld_x, (long)rows, (int)width, l.tx,
+    auto *k = width < Vec<T>::n ? quantize_rows<T, 1, false> : l.hold == 1 ? quantize_rows<T, 1, true> : l.hold == 2 ? quantize_rows<T, 2, true> : quantize_rows<T, 4, true>;
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kThreads), 0, stream, static_cast<const T *>(x), (long)ld_x, (long)rows, (int)width, l.tx,
                        q, (long)ld_q, scale);
     return launched("quantize_rows launch");
 }
@@ -498,11 +590,12 @@ template <typename T>
 int run_combine(const void *rows, int64_t ld_rows, const float *weight, const int32_t *row_of_slot, int64_t tokens, int k, int64_t width, void *y,
                 int64_t ld_y, hipStream_t stream)
 {
-    const int64_t vecs = (width + Vec<T>::n - 1) / Vec<T>::n;
-    const Lay l = lay_out(vecs);
+    const int64_t pieces = (width + Vec<T>::n - 1) / Vec<T>::n;
+    const Lay l = lay_out(pieces, tokens, 1);
     const int64_t blocks = (tokens + l.ty - 1) / l.ty;
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((vecs + l.tx - 1) / l.tx, 1024 / blocks));
-    hipLaunchKernelGGL(route_combine<T>, dim3((unsigned)blocks, (unsigned)parts), dim3(kThreads), 0, stream, static_cast<const T *>(rows), (long)ld_rows, weight,
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((pieces + l.tx - 1) / l.tx, 1024 / blocks));
+    auto *kernel = width < Vec<T>::n ? route_combine<T, false> : route_combine<T, true>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, (unsigned)parts), dim3(kThreads), 0, stream, static_cast<const T *>(rows), (long)ld_rows, weight,
                        row_of_slot, (long)tokens, k, (int)width, l.tx, static_cast<T *>(y), (long)ld_y);
     return launched("route_combine launch");
 }
@@ -510,9 +603,10 @@ template <typename T>
 int run_combine_grad(const void *dy, int64_t ld_dy, const void *rows, int64_t ld_rows, const float *weight, const int32_t *row_of_slot, const int32_t *held_at,
                      int64_t tokens, int k, int64_t width, void *drows, int64_t ld_drows, float *dweight, hipStream_t stream)
 {
-    const Lay l = lay_out((width + Vec<T>::n - 1) / Vec<T>::n);
+    const Lay l = lay_out((width + Vec<T>::n - 1) / Vec<T>::n, tokens, 1);
     const int64_t blocks = (tokens + l.ty - 1) / l.ty;
-    hipLaunchKernelGGL(route_combine_grad<T>, dim3((unsigned)blocks), dim3(kThreads), 0, stream, static_cast<const T *>(dy), (long)ld_dy, static_cast<const T *>(rows),
+    auto *kernel = width < Vec<T>::n ? route_combine_grad<T, false> : route_combine_grad<T, true>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, static_cast<const T *>(dy), (long)ld_dy, static_cast<const T *>(rows),
                        (long)ld_rows, weight, row_of_slot, held_at, (long)tokens, k, (int)width, l.tx, static_cast<T *>(drows), (long)ld_drows, dweight);
     return launched("route_combine_grad launch");
 }
@@ -551,7 +645,7 @@ extern "C" int opevo_route_dispatch(const int32_t *expert, int64_t tokens, int k
     if (int rc = check_dispatch(who, expert, tokens, k, experts, x, ld_x, dtype, width, offsets, row_of_slot)) return rc;
     if (tokens > 0)
         if (int rc = check_rows(who, "rows", rows, ld_rows, width, size_of(dtype))) return rc;
-    Route r;
+    Route r = {};
     const hipStream_t on = static_cast<hipStream_t>(stream);
     if (int rc = plan_route(who, expert, tokens, k, experts, offsets, row_of_slot, workspace, workspace_bytes, on, &r)) return rc;
     return BY_DTYPE(dtype, run_dispatch, r, x, ld_x, width, rows, ld_rows, on);
@@ -567,7 +661,7 @@ extern "C" int opevo_route_dispatch_i8(const int32_t *expert, int64_t tokens, in
         if (int rc = check_rows(who, "q", q, ld_q, width, 1)) return rc;
         if (int rc = check_words(who, "scale", scale)) return rc;
     }
-    Route r;
+    Route r = {};
     const hipStream_t on = static_cast<hipStream_t>(stream);
     if (int rc = plan_route(who, expert, tokens, k, experts, offsets, row_of_slot, workspace, workspace_bytes, on, &r)) return rc;
     return BY_DTYPE(dtype, run_dispatch_i8, r, x, ld_x, width, q, ld_q, scale, on);
