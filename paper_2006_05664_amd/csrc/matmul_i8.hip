@@ -490,33 +490,36 @@ int run_thin(const Product &p, hipStream_t stream)
 
 // A kernel and what it takes, in us: launch + max(steps * chain, load * (tile + steps * rate)), where steps is how many slabs (thin: steps of 256 values) a wave
 // goes through and load the workgroups for each of the 256 compute units, rounded up where one fills a unit.  The first term is a workgroup's chain of latencies,
-// the second what a compute unit gets through.  The constants were fitted to the times of every kernel at 350 (rows apart by multiples of 16) and 250 (others)
-// random sizes of 1 - 8192 rows, 64 - 8192 columns and K of 64 - 8192; the kernel chosen by them took 1.6 % and 2.7 % more than the best of all of them in the
+// the second what a compute unit gets through.  The constants were fitted to the times of every kernel at 400 (rows apart by multiples of 16) and 250 (others)
+// random sizes of 1 - 8192 rows, 64 - 8192 columns and K of 64 - 8192; the kernel chosen by them took 0.8 % and 2.7 % more than the best of all of them in the
 // geometric mean, at most 1.4 times as much.
 struct Kernel {
     int (*run)(const Product &, hipStream_t);
     int bm, bn, step, ways;             // tile, K of a step, waves or groups that share the steps
-    bool round_up, thin;
+    int64_t most;                       // rows it is considered for
+    bool round_up;
     float launch, chain, tile, rate;
 };
+constexpr int64_t kAll = INT64_MAX;
 const Kernel kDirect[] = {
-    {run_tile<Shape<true, 256, 256, 2, 4, 2>>, 256, 256, 128, 1, true, false, 0.8f, 1.3f, 8.7f, 1.14f},
-    {run_tile<Shape<true, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, false, false, 2.85f, 1.03f, 2.05f, 0.58f},
-    {run_tile<Shape<true, 128, 128, 2, 4, 4>>, 128, 128, 128, 1, true, false, 0.f, 0.f, 4.85f, 0.466f},
-    {run_tile<Shape<true, 64, 64, 2, 4, 4>>, 64, 64, 128, 1, false, false, 2.89f, 0.294f, 0.466f, 0.296f},
-    {run_tile<Shape<true, 32, 64, 1, 4, 4, 2>>, 32, 64, 128, 2, false, false, 2.77f, 0.388f, 1.3f, 0.507f},
-    {run_tile<Shape<true, 32, 32, 2, 2, 6, 2>>, 32, 32, 128, 2, false, false, 2.45f, 0.252f, 0.654f, 0.352f},
-    {run_thin<1, 1, 4>, 16, 16, 256, 4, false, true, 2.29f, 0.585f, 0.f, 0.958f},
+    {run_tile<Shape<true, 256, 256, 2, 4, 2>>, 256, 256, 128, 1, kAll, true, 0.f, 1.6f, 10.8f, 1.41f},
+    {run_tile<Shape<true, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, kAll, false, 3.03f, 0.844f, 2.47f, 0.66f},
+    {run_tile<Shape<true, 128, 128, 2, 4, 4>>, 128, 128, 128, 1, kAll, true, 0.f, 0.f, 5.18f, 0.576f},
+    {run_tile<Shape<true, 128, 64, 4, 2, 3>>, 128, 64, 128, 1, kAll, false, 2.76f, 0.383f, 1.24f, 0.544f},
+    {run_tile<Shape<true, 64, 64, 2, 4, 4>>, 64, 64, 128, 1, kAll, false, 2.6f, 0.322f, 0.783f, 0.322f},
+    {run_tile<Shape<true, 32, 128, 1, 4, 4>>, 32, 128, 128, 1, kAll, false, 2.92f, 0.269f, 0.802f, 0.431f},
+    {run_tile<Shape<true, 32, 64, 1, 4, 4, 2>>, 32, 64, 128, 2, kAll, false, 2.72f, 0.371f, 1.27f, 0.462f},
+    {run_tile<Shape<true, 32, 32, 2, 2, 6, 2>>, 32, 32, 128, 2, kAll, false, 2.39f, 0.26f, 0.532f, 0.372f},
+    {run_thin<1, 1, 4>, 16, 16, 256, 4, 256, false, 2.22f, 0.683f, 0.f, 0.775f},
 };
 const Kernel kAny[] = {
-    {run_tile<Shape<false, 128, 256, 2, 4, 2>>, 128, 256, 128, 1, true, false, 0.f, 0.f, 7.04f, 1.45f},
-    {run_tile<Shape<false, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, false, false, 3.84f, 0.99f, 3.87f, 1.1f},
-    {run_tile<Shape<false, 64, 64, 2, 4, 2>>, 64, 64, 128, 1, false, false, 3.01f, 0.503f, 1.22f, 0.477f},
-    {run_tile<Shape<false, 32, 32, 2, 2, 2, 2>>, 32, 32, 128, 2, false, false, 2.72f, 0.422f, 0.472f, 0.418f},
-    {run_tile<Shape<false, 32, 32, 2, 2, 2, 4>>, 32, 32, 128, 4, false, false, 2.51f, 0.779f, 0.834f, 0.86f},
-    {run_thin<1, 1, 4>, 16, 16, 256, 4, false, true, 1.17f, 2.01f, 0.f, 2.19f},
+    {run_tile<Shape<false, 128, 256, 2, 4, 2>>, 128, 256, 128, 1, kAll, true, 0.f, 0.f, 7.04f, 1.45f},
+    {run_tile<Shape<false, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, kAll, false, 3.84f, 0.99f, 3.87f, 1.1f},
+    {run_tile<Shape<false, 64, 64, 2, 4, 2>>, 64, 64, 128, 1, kAll, false, 3.01f, 0.503f, 1.22f, 0.477f},
+    {run_tile<Shape<false, 32, 32, 2, 2, 2, 2>>, 32, 32, 128, 2, kAll, false, 2.72f, 0.422f, 0.472f, 0.418f},
+    {run_tile<Shape<false, 32, 32, 2, 2, 2, 4>>, 32, 32, 128, 4, kAll, false, 2.51f, 0.779f, 0.834f, 0.86f},
+    {run_thin<1, 1, 4>, 16, 16, 256, 4, 64, false, 1.17f, 2.01f, 0.f, 2.19f},
 };
-constexpr int64_t kThinRows = 64;       // beyond, the 16 rows of a thin tile read the weights too often
 
 int run_product(const Product &p, hipStream_t stream)
 {
@@ -530,7 +533,7 @@ int run_product(const Product &p, hipStream_t stream)
     const Kernel *best = nullptr;
     float least = 0.f;
     const auto consider = [&](const Kernel &k) {
-        if (k.thin && rows > kThinRows) return;
+        if (rows > k.most) return;
         const int64_t groups = parts * ((rows + k.bm - 1) / k.bm) * ((p.n + k.bn - 1) / k.bn), slabs = (p.k + k.step - 1) / k.step;
         const float steps = (float)((slabs + k.ways - 1) / k.ways), load = k.round_up ? (float)((groups + 255) / 256) : (float)groups / 256.f;
         const float us = k.launch + std::max(steps * k.chain, load * (k.tile + steps * k.rate));
