@@ -80,12 +80,12 @@ __device__ __forceinline__ bool find_rows(const Product &p, int bm, long tile, R
 // rows as its first operand).  Stored like that, an instruction would touch 16 rows, 32 bytes of each, and the scales would be loaded under a mask for every atom
 // (8192 x 4096 x 1024: 77 us, 27 of them for each tile's epilogue); the 16 rows of an atom row go through a piece of LDS of the wave's own instead and leave as whole
 // lines, 16 bytes a lane.
-template <typename T, int NI> constexpr int kPatch = 16 * (NI * 16 * (int)sizeof(T) + 16);   // bytes of LDS a wave takes
+template <typename T, int NI> constexpr int kPatch = 16 * NI * 16 * (int)sizeof(T);   // bytes of LDS a wave takes
 template <typename T, int MI, int NI>
-__device__ __forceinline__ void store_tile(const Product &p, const Rows &r, int m0, int col0, const i32x4 (&acc)[MI][NI], int8_t *patch)
+__device__ __forceinline__ void store_tile(const Product &p, const Rows &r, int m0, int col0, const i32x4 (&acc)[MI][NI], int8_t *patch, int lane)
 {
-    constexpr int PITCH = NI * 16 * (int)sizeof(T) + 16, CPR = NI * (int)sizeof(T), V = 16 / (int)sizeof(T);   // bytes, 16-byte chunks of a row, elements of a chunk
-    const int lane = threadIdx.x & 63, cols = p.n - col0;
+    constexpr int PITCH = NI * 16 * (int)sizeof(T), CPR = NI * (int)sizeof(T), V = 16 / (int)sizeof(T);   // bytes, 16-byte chunks of a row, elements of a chunk
+    const int cols = p.n - col0;
     const float *sbp = p.sb + (long)r.expert * p.n + col0;
     float sb[NI][4], sa[MI];
 #pragma unroll
@@ -108,7 +108,9 @@ __device__ __forceinline__ void store_tile(const Product &p, const Rows &r, int 
             T v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = narrow<T>((float)acc[i][j][e] * (sa[i] * sb[j][e]));
-            __builtin_memcpy(__builtin_assume_aligned(patch + (lane & 15) * PITCH + (j * 16 + (lane >> 4) * 4) * sizeof(T), 4 * sizeof(T)), v, sizeof v);
+            constexpr int OF = 16 / (4 * (int)sizeof(T));       // such pieces of a chunk
+            const int piece = j * 4 + (lane >> 4), chunk = (piece / OF) ^ (lane & 15) % CPR;     // a row's chunks are permuted, so that 16 rows fall on different banks
+            __builtin_memcpy(__builtin_assume_aligned(patch + (lane & 15) * PITCH + chunk * 16 + piece % OF * (16 / OF), 4 * sizeof(T)), v, sizeof v);
         }
         __builtin_amdgcn_wave_barrier();
         const long row0 = r.first + m0 + i * 16;
@@ -118,15 +120,11 @@ __device__ __forceinline__ void store_tile(const Product &p, const Rows &r, int 
             if ((16 * CPR) % 64 != 0 && row >= 16) continue;
             if (row0 + row >= r.last || c >= cols) continue;
             T *dst = (T *)p.c + (row0 + row) * p.ldc + col0 + c;
-            const i32x4 w = *(const i32x4 *)(patch + row * PITCH + at % CPR * 16);
-            if (c + V <= cols) __builtin_memcpy(dst, &w, 16);
-            else {
-                T part[V];
-                __builtin_memcpy(part, &w, 16);
-#pragma unroll
-                for (int e = 0; e < V; ++e)
-                    if (c + e < cols) dst[e] = part[e];
-            }
+            const int8_t *from = patch + row * PITCH + (at % CPR ^ row % CPR) * 16;
+            if (c + V <= cols) __builtin_memcpy(dst, __builtin_assume_aligned(from, 16), 16);
+            else
+#pragma unroll 1
+                for (int e = 0; e < cols - c; ++e) dst[e] = ((const T *)from)[e];
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -461,9 +459,9 @@ void product_tile(Product p)
         if (group > 0) return;
     }
     int8_t *const patch = whole + wave * kPatch<float, NI>;
-    if (p.out == OPEVO_F32) store_tile<float>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch);
-    else if (p.out == OPEVO_BF16) store_tile<__bf16>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch);
-    else store_tile<_Float16>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch);
+    if (p.out == OPEVO_F32) store_tile<float>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch, lane);
+    else if (p.out == OPEVO_BF16) store_tile<__bf16>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch, lane);
+    else store_tile<_Float16>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch, lane);
 }
 
 using opevo::fail;
