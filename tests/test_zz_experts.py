@@ -319,6 +319,60 @@ def test_products(M, N, K, dtype, pa, pb, pc, shift):
     _check_product(c.host(), av, bv, sa, sb, dtype)
 
 
+# M, N, K, output: sizes at which every kernel is the one chosen, with ragged tiles, K that ends inside a slab (multiples of 16 and others), one slab and many
+LARGE = [
+    (2700, 4300, 1040, "bf16"), (2691, 4374, 32, "f32"), (600, 3900, 1168, "f16"), (515, 2770, 144, "f32"), (1950, 2050, 1200, "bf16"), (2040, 2030, 1616, "f32"),
+    (3272, 1052, 32, "bf16"), (700, 1900, 720, "f32"), (194, 3354, 32, "f16"), (900, 1000, 1040, "bf16"), (270, 523, 32, "f32"), (632, 520, 832, "bf16"),
+    (1023, 325, 1808, "f32"), (453, 549, 1552, "f16"), (190, 250, 2000, "f32"), (150, 900, 1040, "bf16"), (9, 300, 1616, "f32"), (250, 100, 1616, "f16"),
+    (2900, 4200, 1001, "bf16"), (1801, 2077, 1001, "f32"), (1801, 2077, 21, "f16"), (1500, 1100, 777, "bf16"), (477, 3836, 22, "f32"), (600, 900, 645, "f16"),
+    (36, 4163, 20, "bf16"), (60, 450, 1111, "f32"), (70, 36, 1700, "bf16"), (95, 40, 279, "f32"), (12, 390, 1394, "f16"), (1, 52, 413, "bf16"),
+]
+
+
+@gpu
+@pytest.mark.parametrize("M,N,K,dtype", LARGE)
+@pytest.mark.parametrize("pad", [0, 16, 3])
+def test_large_products(M, N, K, dtype, pad):
+    torch, _ = _torch()
+    g = torch.Generator(device="cuda").manual_seed(M + N + K)
+    a, b, c = Matrix(M, K, "i8", K + pad), Matrix(N, K, "i8", K + pad), Matrix(M, N, dtype, N + pad)
+    for m in (a, b):
+        m.view.copy_(torch.randint(-128, 128, (m.rows, K), generator=g, device="cuda", dtype=torch.int8))
+    sa, sb = torch.rand(M, generator=g, device="cuda") * 1e-2, torch.rand(N, generator=g, device="cuda") * 1e-2
+    P.opevo_matmul_i8(a.ptr, a.ld, sa.data_ptr(), b.ptr, b.ld, sb.data_ptr(), c.ptr, c.ld, CODE[dtype], M, N, K)
+    exact = (torch.matmul(a.view.double(), b.view.double().t().contiguous()) * sa.double()[:, None] * sb.double()).cpu().numpy()
+    assert np.all(np.abs(c.host() - exact) <= (3 * U + V[dtype] * (1 + 4 * U)) * np.abs(exact) + TINY[dtype])
+
+
+LARGE_GROUPS = [
+    ([900, 0, 1411, 300, 2000, 77], 50, 2050, 400, "bf16"), ([300, 5, 0, 130], 3, 2200, 272, "f32"), ([700, 900, 0, 400], 60, 1700, 656, "f16"), ([128, 0, 260, 400], 11, 1300, 784, "f32"),
+    ([100, 3, 300, 80], 9, 560, 416, "bf16"), ([40, 0, 90, 2], 4, 1980, 528, "f32"), ([200, 180, 200], 7, 560, 1104, "f16"), ([20, 0, 1, 40], 5, 300, 1040, "bf16"),
+    ([300, 250], 20, 500, 784, "f32"), ([900, 0, 411, 500], 77, 1300, 501, "bf16"), ([300, 0, 900, 200], 20, 1300, 270, "f32"), ([150, 60, 200], 9, 700, 333, "f16"),
+    ([410, 200, 0], 5, 573, 145, "f32"), ([20, 1, 0, 14], 2, 100, 275, "bf16"), ([100, 48], 9, 70, 900, "f32"), ([30, 1, 0, 9], 6, 60, 815, "bf16"),
+]
+
+
+@gpu
+@pytest.mark.parametrize("counts,none,N,K,dtype", LARGE_GROUPS)
+def test_large_products_of_experts(counts, none, N, K, dtype):
+    torch, _ = _torch()
+    E, rows, g = len(counts), sum(counts) + none, torch.Generator(device="cuda").manual_seed(N + K)
+    a, b, c = Matrix(rows, K, "i8"), Matrix(E * N, K, "i8"), Matrix(rows, N, dtype)
+    for m in (a, b):
+        m.view.copy_(torch.randint(-128, 128, (m.rows, K), generator=g, device="cuda", dtype=torch.int8))
+    sa, sb = torch.rand(rows, generator=g, device="cuda") * 1e-2, torch.rand(E * N, generator=g, device="cuda") * 1e-2
+    offsets = np.concatenate([[0], np.cumsum(counts)])
+    sa[int(offsets[-1]):] = float("inf")
+    d_off = _words(offsets, np.int32)
+    P.opevo_matmul_i8_grouped(a.ptr, K, sa.data_ptr(), b.ptr, K, sb.data_ptr(), d_off.data_ptr(), E, c.ptr, N, CODE[dtype], rows, N, K)
+    got = c.host()
+    assert not got[offsets[-1]:].any()
+    for e in range(E):
+        part, own = slice(offsets[e], offsets[e + 1]), slice(e * N, (e + 1) * N)
+        exact = (torch.matmul(a.view[part].double(), b.view[own].double().t().contiguous()) * sa[part].double()[:, None] * sb[own].double()).cpu().numpy()
+        assert np.all(np.abs(got[part] - exact) <= (3 * U + V[dtype] * (1 + 4 * U)) * np.abs(exact) + TINY[dtype]), e
+
+
 @gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("M,N,K", [(1, 500, 512), (40, 300, 200), (300, 700, 256)])
@@ -504,6 +558,22 @@ def test_layer_in_a_graph_and_on_another_stream():
         torch.cuda.synchronize()
         for name in eager:
             assert torch.equal(eager[name], recorded[name]), (seed, name)
+
+
+@gpu
+def test_example_layer():
+    """The example's layer against 64 bits.  Trained: sums of at most 1024 fp32 products of either sign, far below 1e-4.  Served: tokens, hidden values and both weights are
+    rounded to 127 steps of their row's largest, about 3.5 to 4.5 standard deviations of normal values (a step of 0.035, off by 0.035 / sqrt 12 = 1 % each), and the hidden rows, half of
+    them zeros, alike: two factors a product and two products, sqrt 4 * 1 % = 2 %, twice that allowed."""
+    _torch()
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "expert_layer.py")
+    spec = importlib.util.spec_from_file_location("expert_layer", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    for name, error in example.main(tokens=300, k=3, experts=7, width=256, inner=520).items():
+        assert error <= (4e-2 if name.startswith("served") else 1e-4), (name, error)
 
 
 def _refused(text, call, *args):
