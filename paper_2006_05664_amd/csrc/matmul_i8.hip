@@ -29,6 +29,10 @@ struct Product {
     int n, k;
 };
 
+// A grid's second extent ends at 65535: tiles of rows go on in the third.
+constexpr int kGridY = 65535;
+__device__ __forceinline__ long row_tile() { return (long)blockIdx.z * kGridY + blockIdx.y; }
+
 // The rows a workgroup owns, of one expert.
 struct Rows { long first, last; int expert; bool zero; };
 
@@ -169,7 +173,7 @@ void product_thin(Product p)
 {
     __shared__ i32x4 sums[W][MI * NI][64];
     Rows r;
-    if (!find_rows(p, MI * 16, blockIdx.y, &r)) return;
+    if (!find_rows(p, MI * 16, row_tile(), &r)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n0 = blockIdx.x * NI * 16;
     i32x4 acc[MI][NI] = {};
     if (!r.zero) {
@@ -284,7 +288,7 @@ void product_tile(Product p)
     __shared__ __attribute__((aligned(1024))) int8_t whole[S::KG * S::STAGES * S::STAGE];
     static_assert(S::NW * kPatch<float, NI> <= S::KG * S::STAGES * S::STAGE && (S::KG - 1) * S::NW * MI * NI * 1024 <= S::KG * S::STAGES * S::STAGE, "");
     Rows r;
-    if (!find_rows(p, BM, blockIdx.y, &r)) return;
+    if (!find_rows(p, BM, row_tile(), &r)) return;
     const int tid = threadIdx.x, lane = tid & 63, all = uniform(tid >> 6), group = all / S::NW, wave = all % S::NW, wm = wave / S::WN, wn = wave % S::WN;
     const int n0 = blockIdx.x * BN;
     int8_t *const ring = whole + group * (S::STAGES * S::STAGE);
@@ -469,10 +473,16 @@ using opevo::fail;
 // How many tiles of bm rows there can be at most.  Grouped: each expert's last one is ragged, and so is that of the rows of none.
 int64_t row_tiles(const Product &p, int bm) { return p.offsets ? std::min<int64_t>(p.m, p.m / bm + p.experts + 1) : (p.m + bm - 1) / bm; }
 
+dim3 grid_of(const Product &p, int bm, int bn)
+{
+    const int64_t tiles = row_tiles(p, bm);
+    return dim3((unsigned)((p.n + bn - 1) / bn), (unsigned)std::min<int64_t>(tiles, kGridY), (unsigned)((tiles + kGridY - 1) / kGridY));
+}
+
 template <typename S>
 int run_tile(const Product &p, hipStream_t stream)
 {
-    hipLaunchKernelGGL(product_tile<S>, dim3((unsigned)((p.n + S::BN - 1) / S::BN), (unsigned)row_tiles(p, S::BM)), dim3(S::NT), 0, stream, p);
+    hipLaunchKernelGGL(product_tile<S>, grid_of(p, S::BM, S::BN), dim3(S::NT), 0, stream, p);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? OPEVO_OK : opevo::hip_fail(e, "product launch");
 }
@@ -480,8 +490,7 @@ int run_tile(const Product &p, hipStream_t stream)
 template <int MI, int NI, int W>
 int run_thin(const Product &p, hipStream_t stream)
 {
-    constexpr int BM = MI * 16, BN = NI * 16;
-    hipLaunchKernelGGL((product_thin<MI, NI, W>), dim3((unsigned)((p.n + BN - 1) / BN), (unsigned)row_tiles(p, BM)), dim3(W * 64), 0, stream, p);
+    hipLaunchKernelGGL((product_thin<MI, NI, W>), grid_of(p, MI * 16, NI * 16), dim3(W * 64), 0, stream, p);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? OPEVO_OK : opevo::hip_fail(e, "product launch");
 }

@@ -125,6 +125,7 @@ ROUTES = [
     (4097, 1, 1, 8, "f32", 1.0, 0, 0),          # one expert takes all
     (4500, 7, 1000, 40, "f16", 0.95, 0, 0),
     (20011, 2, 13, 72, "bf16", 0.9, 8, 0),
+    (150001, 2, 777, 8, "f16", 0.97, 0, 0),
 ]
 
 
@@ -342,6 +343,17 @@ def test_large_products(M, N, K, dtype, pad):
     P.opevo_matmul_i8(a.ptr, a.ld, sa.data_ptr(), b.ptr, b.ld, sb.data_ptr(), c.ptr, c.ld, CODE[dtype], M, N, K)
     exact = (torch.matmul(a.view.double(), b.view.double().t().contiguous()) * sa.double()[:, None] * sb.double()).cpu().numpy()
     assert np.all(np.abs(c.host() - exact) <= (3 * U + V[dtype] * (1 + 4 * U)) * np.abs(exact) + TINY[dtype])
+
+
+@gpu
+@pytest.mark.parametrize("M,N,K,ldb", [(1 << 21, 3, 16, 16), ((1 << 21) - 7, 40, 16, 16), (1100000, 2, 40, (1 << 24) + 16), (1100001, 5, 13, 13)])
+def test_more_rows_than_a_grid_has_in_one_extent(M, N, K, ldb):
+    torch, _ = _torch()
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    a, b, ones = torch.randint(-128, 128, (M, K), generator=g, device="cuda", dtype=torch.int8), torch.randint(-128, 128, (N, ldb), generator=g, device="cuda", dtype=torch.int8), torch.ones(M, device="cuda")
+    c = torch.full((M, N), float("nan"), device="cuda")
+    P.opevo_matmul_i8(a.data_ptr(), K, ones.data_ptr(), b.data_ptr(), ldb, ones.data_ptr(), c.data_ptr(), N, P.OPEVO_F32, M, N, K)
+    assert torch.equal(c, torch.matmul(a.float(), b[:, :K].float().t().contiguous()))
 
 
 LARGE_GROUPS = [
