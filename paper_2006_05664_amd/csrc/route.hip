@@ -90,7 +90,7 @@ __device__ __forceinline__ void route_rows(const Route &r, long first_slot, int 
     for (int e = tid; e < r.experts; e += kThreads) s.total[e] = s.before[e] = 0;
     __syncthreads();
     if (r.counts) {
-        const int at = (int)(first_slot / r.chunk);
+        const int at = (int)(first_slot >> __builtin_ctz(r.chunk));     // chunks are powers of two
         const int lines = kThreads / r.experts > 1 ? kThreads / r.experts : 1, line = lines > 1 ? tid / r.experts : 0;
         for (int e = lines > 1 ? tid - line * r.experts : tid; e < r.experts && line < lines; e += kThreads) {
             int total = 0, before = 0;
@@ -176,7 +176,7 @@ void route_dispatch(Route r, const T *__restrict__ x, long ld_x, int width, int 
     const long first = (long)blockIdx.x * r.tokens_per_block;
     const int tokens = (int)(r.tokens - first < r.tokens_per_block ? r.tokens - first : r.tokens_per_block), own = tokens * r.k;
     const Pieces<T, WIDE> at(width);
-    const int lane = threadIdx.x % tx, ty = kThreads / tx, line = threadIdx.x / tx;
+    const int lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx), line = (int)threadIdx.x >> __builtin_ctz(tx);
     const int step = tx * gridDim.y * kHold, start = blockIdx.y * tx * kHold + lane;
     Vec<T> v[kHold], w[kHold];
     auto load = [&](Vec<T> (&to)[kHold], int t, int c) {
@@ -281,7 +281,7 @@ __device__ __forceinline__ unsigned row_max(unsigned m, int tx, unsigned *red)
         __syncthreads();
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
         __syncthreads();
-        const int w0 = threadIdx.x / tx * (tx / 64);
+        const int w0 = (threadIdx.x >> __builtin_ctz(tx)) * (tx / 64);
         for (int w = 0; w < tx / 64; ++w) m = max(m, red[w0 + w]);
     }
     return m;
@@ -321,8 +321,8 @@ __global__ __launch_bounds__(kThreads)
 void quantize_rows(const T *__restrict__ x, long ld_x, long rows, int width, int tx, int8_t *__restrict__ q, long ld_q, float *__restrict__ scale)
 {
     __shared__ unsigned red[kThreads / 64];
-    const int lane = threadIdx.x % tx, ty = kThreads / tx;
-    const long row = (long)blockIdx.x * ty + threadIdx.x / tx;
+    const int lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx);
+    const long row = (long)blockIdx.x * ty + ((int)threadIdx.x >> __builtin_ctz(tx));
     const bool on = row < rows;
     const T *src = x + (on ? row : 0) * ld_x;
     const Pieces<T, WIDE> at(width);
@@ -348,7 +348,7 @@ void route_dispatch_i8(Route r, const T *__restrict__ x, long ld_x, int width, i
     __shared__ unsigned red[kThreads / 64];
     const long first = (long)blockIdx.x * r.tokens_per_block;
     const int tokens = (int)(r.tokens - first < r.tokens_per_block ? r.tokens - first : r.tokens_per_block), own = tokens * r.k;
-    const int lane = threadIdx.x % tx, ty = kThreads / tx, line = threadIdx.x / tx;
+    const int lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx), line = (int)threadIdx.x >> __builtin_ctz(tx);
     const Pieces<T, WIDE> at(width);
     Held<T, kHold, WIDE> h, next;
     h.load(at, x + (first + line) * ld_x, lane, tx, line < tokens);
@@ -395,8 +395,8 @@ __global__ __launch_bounds__(kThreads)
 void route_combine(const T *__restrict__ rows, long ld_rows, const float *__restrict__ weight, const int *__restrict__ row_of_slot,
                    long tokens, int k, int width, int tx, T *__restrict__ y, long ld_y)
 {
-    const int lane = threadIdx.x % tx, ty = kThreads / tx;
-    const long t = (long)blockIdx.x * ty + threadIdx.x / tx, slots = tokens * k;
+    const int lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx);
+    const long t = (long)blockIdx.x * ty + ((int)threadIdx.x >> __builtin_ctz(tx)), slots = tokens * k;
     if (t >= tokens) return;
     const Pieces<T, WIDE> at(width);
     for (int i = blockIdx.y * tx + lane; i < at.count; i += tx * gridDim.y) {
@@ -441,7 +441,7 @@ void route_combine_grad(const T *__restrict__ dy, long ld_dy, const T *__restric
 {
     __shared__ float red[OPEVO_ROUTE_MAX_SLOTS][kThreads / 64];
     const int j0 = blockIdx.y * share, j1 = min(k, j0 + share);
-    const int lane = threadIdx.x % tx, ty = kThreads / tx, line = threadIdx.x / tx;
+    const int lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx), line = (int)threadIdx.x >> __builtin_ctz(tx);
     const long t = (long)blockIdx.x * ty + line, slots = tokens * k;
     const bool on = t < tokens;
     const Pieces<T, WIDE> at(width);
