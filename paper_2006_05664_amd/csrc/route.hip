@@ -56,12 +56,18 @@ __global__ __launch_bounds__(kThreads)
 void route_count(const int *__restrict__ expert, long slots, int chunk, int experts, int *__restrict__ counts)
 {
     __shared__ int hist[kMaxExperts];
-    for (int e = threadIdx.x; e < experts; e += kThreads) hist[e] = 0;
-    __syncthreads();
     const long first = (long)blockIdx.x * chunk, last = first + chunk < slots ? first + chunk : slots;
-    for (long s = first + threadIdx.x; s < last; s += kThreads) {
-        const unsigned e = expert[s];
-        if (e < (unsigned)experts) atomicAdd(&hist[e], 1);
+    for (long s0 = first; s0 < last; s0 += kThreads * 4) {
+        unsigned e[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) e[u] = s0 + u * kThreads + threadIdx.x < last ? (unsigned)expert[s0 + u * kThreads + threadIdx.x] : ~0u;
+        if (s0 == first) {                  // while the first ones come
+            for (int i = threadIdx.x; i < experts; i += kThreads) hist[i] = 0;
+            __syncthreads();
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (e[u] < (unsigned)experts) atomicAdd(&hist[e[u]], 1);
     }
     __syncthreads();
     for (int e = threadIdx.x; e < experts; e += kThreads) counts[(long)blockIdx.x * experts + e] = hist[e];
@@ -94,7 +100,7 @@ __device__ __forceinline__ void route_rows(const Route &r, long first_slot, int 
         const int lines = kThreads / r.experts > 1 ? kThreads / r.experts : 1, line = lines > 1 ? tid / r.experts : 0;
         for (int e = lines > 1 ? tid - line * r.experts : tid; e < r.experts && line < lines; e += kThreads) {
             int total = 0, before = 0;
-#pragma unroll 4
+#pragma unroll 16
             for (int c = line; c < r.chunks; c += lines) {
                 const int n = r.counts[c * r.experts + e];
                 total += n;
@@ -103,9 +109,13 @@ __device__ __forceinline__ void route_rows(const Route &r, long first_slot, int 
             atomicAdd(&s.total[e], total);
             atomicAdd(&s.before[e], before);
         }
-        for (long i = (long)at * r.chunk + tid; i < first_slot; i += kThreads) {
-            const unsigned e = r.expert[i];
-            if (e < (unsigned)r.experts) atomicAdd(&s.before[e], 1);
+        for (long i0 = (long)at * r.chunk; i0 < first_slot; i0 += kThreads * 4) {
+            unsigned e[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) e[u] = i0 + u * kThreads + tid < first_slot ? (unsigned)r.expert[i0 + u * kThreads + tid] : ~0u;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (e[u] < (unsigned)r.experts) atomicAdd(&s.before[e[u]], 1);
         }
     } else {
         // both counts in one word, neither beyond 16 bits (kCountAlone slots at most)
@@ -158,8 +168,9 @@ static Lay lay_out(int64_t pieces, int64_t rows, int most)
 {
     int tx = 1, hold = 1;
     while (tx < kThreads && tx < pieces) tx *= 2;
-    while (hold < most && (tx * hold < pieces || (tx > 1 && rows * (tx / 2) / 64 >= 4096))) {
-        if (rows * (tx / 2) / 64 >= 4096 && tx * hold >= pieces) tx /= 2;
+    const auto many = [&] { return tx > 64 && rows * (tx / 2) / 64 >= 4096; };      // a wave to a row at least: its accesses stay whole lines
+    while (hold < most && (tx * hold < pieces || many())) {
+        if (many() && tx * hold >= pieces) tx /= 2;
         hold *= 2;
     }
     return {tx, kThreads / tx, hold};
@@ -526,7 +537,7 @@ constexpr int64_t kCountAlone = 4096;
 int64_t chunk_of(int64_t slots, int experts)
 {
     int64_t chunk = 256;
-    while (chunk < 8192 && 2 * chunk * chunk < slots * experts) chunk *= 2;
+    while (chunk < 8192 && 8 * chunk * chunk < slots * experts) chunk *= 2;
     return chunk;
 }
 
