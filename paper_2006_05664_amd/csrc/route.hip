@@ -73,6 +73,7 @@ void route_count(const int *__restrict__ expert, long slots, int chunk, int expe
     for (int e = threadIdx.x; e < experts; e += kThreads) counts[(long)blockIdx.x * experts + e] = hist[e];
 }
 
+constexpr int kFew = 16;                // slots that one wave sorts by comparing them
 constexpr int kOwn = 64;                // slots of a workgroup at most: one wave ranks them
 
 struct Route {
@@ -84,7 +85,7 @@ struct Route {
     int tokens_per_block;
     int *offsets, *row_of_slot;
 };
-struct Sorted { int total[kMaxExperts], before[kMaxExperts], place[kOwn], held; };
+struct Sorted { __attribute__((aligned(16))) int total[kMaxExperts]; int before[kMaxExperts], place[kOwn], held; };
 
 // Rows of this workgroup's slots into place[] (-1: none), from the slots' experts alone: a slot's row is the number of slots of
 // lower experts, plus the earlier slots of its own.  Earlier slots are those of earlier chunks (counted by route_count, a column sum), those of
@@ -92,7 +93,33 @@ struct Sorted { int total[kMaxExperts], before[kMaxExperts], place[kOwn], held; 
 // held: the number of slots that have a row.
 __device__ __forceinline__ void route_rows(const Route &r, long first_slot, int own, Sorted &s, bool writes)
 {
-    const int tid = threadIdx.x, slot = tid < own ? r.expert[first_slot + tid] : -1;
+    const int tid = threadIdx.x;
+    // A few slots (one token: 2.5 us instead of 3.1; 64 slots take 4.7 this way and 3.6 the other): a lane for each, whose row is the number of smaller keys, a key being the
+    // expert and the slot.
+    if (r.tokens * r.k <= kFew) {
+        if (tid < 64) {
+            const int slots = (int)(r.tokens * r.k), e = tid < slots ? r.expert[tid] : -1;
+            const bool valid = (unsigned)e < (unsigned)r.experts;
+            const int key = valid ? e * 64 + tid : INT32_MAX;
+            s.total[tid] = key;
+            __builtin_amdgcn_wave_barrier();
+            auto smaller = [&](int than) {
+                int n = 0;
+                for (int i = 0; i < slots; i += 4)          // one wave, whose LDS accesses keep their order
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) n += s.total[i + u] < than;
+                return n;
+            };
+            const int at = tid - (int)first_slot, row = smaller(key), held = __popcll(__ballot(valid));
+            if (at >= 0 && at < own) s.place[at] = valid ? row : -1;
+            if (tid == 0) s.held = held;
+            if (writes)
+                for (int i = tid; i <= r.experts; i += 64) r.offsets[i] = smaller(i * 64);
+        }
+        __syncthreads();
+        return;
+    }
+    const int slot = tid < own ? r.expert[first_slot + tid] : -1;
     for (int e = tid; e < r.experts; e += kThreads) s.total[e] = s.before[e] = 0;
     __syncthreads();
     if (r.counts) {

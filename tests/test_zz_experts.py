@@ -118,6 +118,9 @@ ROUTES = [
     (1, 2, 8, 64, "f32", 0.0, 0, 0),            # nothing is held here
     (3, 64, 1024, 7, "f16", 0.9, 2, 1),         # every slot a token can have, every expert there can be
     (5, 3, 4, 17, "f32", 0.8, 3, 1),
+    (2, 8, 1000, 33, "bf16", 0.8, 0, 0),
+    (16, 1, 65, 100, "f16", 0.7, 0, 0),
+    (17, 1, 64, 100, "f32", 0.7, 0, 0),
     (33, 8, 40, 1001, "f16", 0.75, 0, 0),
     (64, 2, 64, 8200, "bf16", 1.0, 0, 0),       # rows longer than a workgroup holds in one go
     (257, 5, 9, 130, "bf16", 0.5, 1, 3),
