@@ -89,6 +89,7 @@ template <typename T, int MI, int NI>
 __device__ __forceinline__ void store_tile(const Product &p, const Rows &r, int m0, int col0, const i32x4 (&acc)[MI][NI], int8_t *patch, int lane)
 {
     constexpr int PITCH = NI * 16 * (int)sizeof(T), CPR = NI * (int)sizeof(T), V = 16 / (int)sizeof(T);   // bytes, 16-byte chunks of a row, elements of a chunk
+    static_assert((CPR & (CPR - 1)) == 0, "chunks are permuted by an exclusive or");
     const int cols = p.n - col0;
     const float *sbp = p.sb + (long)r.expert * p.n + col0;
     float sb[NI][4], sa[MI];
@@ -166,7 +167,8 @@ __device__ __forceinline__ i32x4 load_chunk(const int8_t *row, int k, int end)
 // ------------------------------------------------------------------ few rows
 // For few rows the weights are all there is to read, each once, and the time is that of one trip to memory.  No LDS and no barrier stands between: every wave loads
 // its fragments from global memory into registers, 256 values along K a step (four MFMA steps), the next step's while it multiplies.  The W waves of a
-// workgroup share a tile of MI x NI atoms and deal the steps among themselves; their sums meet in LDS.  Loads take any alignment.
+// workgroup share a tile of MI x NI atoms and deal the steps among themselves; their sums meet in LDS.  Loads take any alignment.  One row of 4096 x 1024 weights 3.5 us (a launch alone
+// takes 2.3), of 8192 x 8192 15 us = 4.4 TB/s; 16 rows of it 18.  Wider tiles (1 x 2, 2 x 1 and 2 x 2 atoms) and 8 or 16 waves measured the same or slower.
 template <int MI, int NI, int W>
 __global__ __launch_bounds__(W * 64)
 void product_thin(Product p)
@@ -253,6 +255,9 @@ void product_thin(Product p)
 // DIRECT: every wave issues wave-wide loads of 16 bytes a lane whose destination is LDS, eight rows of a slab an instruction, the chunk each lane loads chosen by the
 // permutation; a ring of STAGES slabs keeps STAGES - 1 in flight.  For operands whose pointers, row lengths and K are multiples of 16.
 // Otherwise the slabs pass through registers, from where they start on any address: two stages in LDS, the slab after them on its way.
+// 8192^3: 256 x 256 tiles 416 - 433 us (2540 - 2640 TOP/s), matrix pipes 64 % busy; 386 with zero operands (power), 333 when all rows are the same (memory).  More stages of
+// shorter slabs 455, two workgroups of 256 x 128 a unit 525, 16 waves 732, 4 waves of 128 x 128 597, a workgroup that goes from tile to tile 426; through registers in
+// 128 x 256 tiles 552, and 4095^3, whose rows start anywhere, 114.  1000 x 1000 x 1008 in 64 x 64 tiles 5.7, 1000 x 1000 x 1001 7.6.
 template <bool DIRECT_, int BM_, int BN_, int WM_, int WN_, int STAGES_, int KG_ = 1>
 struct Shape {
     static constexpr bool DIRECT = DIRECT_;

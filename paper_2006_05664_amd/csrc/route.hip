@@ -204,7 +204,7 @@ static Lay lay_out(int64_t pieces, int64_t rows, int most)
 }
 
 // ------------------------------------------------------------------ dispatch
-// Bound by memory: 16384 tokens of 4096 bf16 to two rows each move 403 MB.  A token is read once and written k times; the first pieces are on their way while the slots
+// Bound by memory: 16384 tokens of 4096 bf16 to two rows each move 403 MB in 83 us behind the count's 4.7 (4.6 TB/s in all; a large copy 5.15).  A token is read once and written k times; the first pieces are on their way while the slots
 // are sorted, the next ones while a piece is written.
 template <typename T, int kHold, bool WIDE>
 __global__ __launch_bounds__(kThreads)
@@ -271,7 +271,7 @@ template <> __device__ __forceinline__ float value_of<float>(unsigned m) { retur
 
 // q = round(127 x / a), a the row's largest magnitude.  With 127 x computed first (exact for 16-bit inputs: 11 + 7 bits) and one
 // division, the quotient of two numbers of at most 18 and 11 bits is a tie in fp32 only where it is one exactly, so the result is the
-// rounding of the exact quotient; fp32 inputs may differ from it where the quotient is within 2^-24 of a tie.  A division takes ten instructions: x times 127 / a, off by at most
+// rounding of the exact quotient; fp32 inputs may differ from it where the quotient is within 2^-24 of a tie.  8192 rows of 4096 bf16 take 25 us (4.0 TB/s).  A division takes ten instructions: x times 127 / a, off by at most
 // 2.3e-5 from that, rounds to the same integer unless it is within 4e-5 of a tie, and only then are the piece's eight values divided.
 template <typename T> struct Quantizer {
     float a, pre, inv, scale;
@@ -425,7 +425,7 @@ void route_dispatch_i8(Route r, const T *__restrict__ x, long ld_x, int width, i
 
 // ------------------------------------------------------------------ combine
 // y[t] = sum_j w[t, j] rows[row_of_slot[t, j]], j ascending, in fp32, rounded once; a slot without a row adds nothing, whatever its weight.  Bound by memory: the rows
-// of J slots are on their way together.
+// of J slots are on their way together (8192 tokens, 4 slots, 4096 bf16: 339 MB in 70 - 78 us; J = 8 takes registers that more waves use better: 86).
 constexpr int kSlots = 4;               // J
 
 template <typename T, bool WIDE>
