@@ -330,6 +330,7 @@ LARGE = [
     (1023, 325, 1808, "f32"), (453, 549, 1552, "f16"), (190, 250, 2000, "f32"), (150, 900, 1040, "bf16"), (9, 300, 1616, "f32"), (250, 100, 1616, "f16"),
     (2900, 4200, 1001, "bf16"), (1801, 2077, 1001, "f32"), (1801, 2077, 21, "f16"), (1500, 1100, 777, "bf16"), (477, 3836, 22, "f32"), (600, 900, 645, "f16"),
     (36, 4163, 20, "bf16"), (60, 450, 1111, "f32"), (70, 36, 1700, "bf16"), (95, 40, 279, "f32"), (12, 390, 1394, "f16"), (1, 52, 413, "bf16"),
+    (1043, 1070, 1954, "bf16"), (637, 2395, 1019, "f32"), (41, 5798, 2903, "f16"), (960, 422, 2430, "f32"),
 ]
 
 
@@ -364,6 +365,7 @@ LARGE_GROUPS = [
     ([100, 3, 300, 80], 9, 560, 416, "bf16"), ([40, 0, 90, 2], 4, 1980, 528, "f32"), ([200, 180, 200], 7, 560, 1104, "f16"), ([20, 0, 1, 40], 5, 300, 1040, "bf16"),
     ([300, 250], 20, 500, 784, "f32"), ([900, 0, 411, 500], 77, 1300, 501, "bf16"), ([300, 0, 900, 200], 20, 1300, 270, "f32"), ([150, 60, 200], 9, 700, 333, "f16"),
     ([410, 200, 0], 5, 573, 145, "f32"), ([20, 1, 0, 14], 2, 100, 275, "bf16"), ([100, 48], 9, 70, 900, "f32"), ([30, 1, 0, 9], 6, 60, 815, "bf16"),
+    ([700, 0, 333, 41, 690], 22, 578, 1387, "f16"), ([500, 533, 0], 10, 365, 2361, "bf16"), ([121, 12], 5, 40, 543, "f32"), ([1541, 2101], 10, 1049, 305, "f16"),
 ]
 
 
