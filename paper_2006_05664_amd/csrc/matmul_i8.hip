@@ -254,10 +254,10 @@ void product_thin(Product p)
 // Rows past the end repeat the last one (their results are not stored); chunks past K are zeros.
 // DIRECT: every wave issues wave-wide loads of 16 bytes a lane whose destination is LDS, eight rows of a slab an instruction, the chunk each lane loads chosen by the
 // permutation; a ring of STAGES slabs keeps STAGES - 1 in flight.  For operands whose pointers, row lengths and K are multiples of 16.
-// Otherwise the slabs pass through registers, from where they start on any address: two stages in LDS, the slab after them (of small tiles the two after them) on its way.
+// Otherwise the slabs pass through registers, from where they start on any address: two stages in LDS, the slab after them on its way.
 // 8192^3: 256 x 256 tiles 416 - 433 us (2540 - 2640 TOP/s), matrix pipes 64 % busy; 386 with zero operands (power), 333 when all rows are the same (memory).  More stages of
 // shorter slabs 455, two workgroups of 256 x 128 a unit 525, 16 waves 732, 4 waves of 128 x 128 597, a workgroup that goes from tile to tile 426; through registers in
-// 128 x 256 tiles 552, and 4095^3, whose rows start anywhere, 114.  1000 x 1000 x 1008 in 64 x 64 tiles 5.7, 1000 x 1000 x 999 7.9.
+// 128 x 256 tiles 552, and 4095^3, whose rows start anywhere, 114.  1000 x 1000 x 1008 in 64 x 64 tiles 5.7, 1000 x 1000 x 1001 7.7.
 template <bool DIRECT_, int BM_, int BN_, int WM_, int WN_, int STAGES_, int KG_ = 1>
 struct Shape {
     static constexpr bool DIRECT = DIRECT_;
@@ -332,32 +332,30 @@ void product_tile(Product p)
             }
         };
         // The same by way of registers: fetch starts the loads, put stores what they brought.
-        // Small tiles, whose slabs take less time than a trip to memory, have two slabs on their way; `set` tells them apart.
-        constexpr int DEPTH = !S::DIRECT && MI * NI <= 4 ? 2 : 1;
-        i32x4 hold[DEPTH][PER];
-        auto fetch = [&](int step, int set) {
+        i32x4 hold[PER];
+        auto fetch = [&](int step) {
             const int slab = step * S::KG + group;
             if (slab < whole_slabs) {
 #pragma unroll
-                for (int t = 0; t < PER; ++t) __builtin_memcpy(&hold[set][t], (t < LA ? abase : bbase) + (long)slab * BK + off[t], 16);
+                for (int t = 0; t < PER; ++t) __builtin_memcpy(&hold[t], (t < LA ? abase : bbase) + (long)slab * BK + off[t], 16);
             } else {
 #pragma unroll
                 for (int t = 0; t < PER; ++t) {
                     const int row = (t < LA ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, chunk = (lane & 7) ^ (row >> 1 & 7);
-                    hold[set][t] = load_chunk((t < LA ? abase : bbase) + off[t] - chunk * 16, slab * BK + chunk * 16, p.k);
+                    hold[t] = load_chunk((t < LA ? abase : bbase) + off[t] - chunk * 16, slab * BK + chunk * 16, p.k);
                 }
             }
         };
-        auto put = [&](int stage, int set) {
+        auto put = [&](int stage) {
 #pragma unroll
-            for (int t = 0; t < PER; ++t) *(i32x4 *)(ring + stage * S::STAGE + (t < LA ? (wave * LA + t) * 1024 : BM * BK + (wave * LB + t - LA) * 1024) + lane * 16) = hold[set][t];
+            for (int t = 0; t < PER; ++t) *(i32x4 *)(ring + stage * S::STAGE + (t < LA ? (wave * LA + t) * 1024 : BM * BK + (wave * LB + t - LA) * 1024) + lane * 16) = hold[t];
         };
         // a stage that every wave has read is filled with the slab `step`
-        auto refill = [&](int step, int stage, int set) {
+        auto refill = [&](int step, int stage) {
             if (S::DIRECT) issue(step, stage);
             else {
-                put(stage, set);
-                if (step + DEPTH < steps) fetch(step + DEPTH, set);
+                put(stage);
+                if (step + 1 < steps) fetch(step + 1);
             }
         };
         // this wave has read its part of a slab, and its part of the next one has landed
@@ -369,13 +367,10 @@ void product_tile(Product p)
         // fragments: lane l holds row l % 16, the 16 values from 16 * (l / 16) of a step of 64
         const int sw = lane >> 1 & 7, fr = lane & 15;
         // prologue: slabs 0 .. STAGES - 1 under way, slab 0 landed, its first fragments read
-        if (!S::DIRECT)
-#pragma unroll
-            for (int s = 0; s < DEPTH; ++s)
-                if (s < steps) fetch(s, s);
+        if (!S::DIRECT) fetch(0);
 #pragma unroll
         for (int s = 0; s < S::STAGES; ++s)
-            if (s < steps) refill(s, s, s % DEPTH);
+            if (s < steps) refill(s, s);
         if (!S::DIRECT) WAIT_LGKM();
         else if (S::STAGES > 2 && steps > S::STAGES) WAIT_LGKM_VMCNT((S::STAGES - 1) * PER);
         else WAIT_LGKM_VMCNT(0);
@@ -402,7 +397,7 @@ void product_tile(Product p)
                 wait_next(more);
                 BARRIER();                  // every wave has read slab q, and slab q + 1 has landed
                 read_slab(set ^ 1, next);
-                if (more) refill(q + S::STAGES, stage, DEPTH == 2 ? set : 0);     // two stages: the slab's parity
+                if (more) refill(q + S::STAGES, stage);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int kk = 0; kk < 2; ++kk)
@@ -439,7 +434,7 @@ void product_tile(Product p)
                     if (kk == 1 && m == 0) {
                         wait_next(more);
                         BARRIER();
-                        if (more) refill(q + S::STAGES, stage, 0);
+                        if (more) refill(q + S::STAGES, stage);
                     }
                     const int lo = m * NR / SLOTS, hi = (m + 1) * NR / SLOTS;
 #pragma unroll
@@ -507,9 +502,9 @@ int run_thin(const Product &p, hipStream_t stream)
 
 // A kernel and what it takes, in us: launch + max(steps * chain, load * (tile + steps * rate)), where steps is how many slabs (thin: steps of 256 values) a wave
 // goes through and load the workgroups for each of the 256 compute units, rounded up where that foretold the times better.  The first term is a workgroup's chain of latencies,
-// the second what a compute unit gets through.  The constants were fitted to the times of every kernel at 400 (rows apart by multiples of 16) and 350 (others)
-// random sizes of 1 - 8192 rows, 64 - 8192 columns and K of 64 - 8192; the kernel chosen by them took 0.8 % and 1.4 % more than the best of all of them in the
-// geometric mean, at most 1.45 times as much.
+// the second what a compute unit gets through.  The constants were fitted to the times of every kernel at 400 (rows apart by multiples of 16) and 450 (others)
+// random sizes of 1 - 8192 rows, 64 - 8192 columns and K of 64 - 8192; the kernel chosen by them took 0.8 % and 1.9 % more than the best of all of them in the
+// geometric mean, at most 1.5 times as much.
 struct Kernel {
     int (*run)(const Product &, hipStream_t);
     int bm, bn, step, ways;             // tile, K of a step, waves or groups that share the steps
@@ -530,14 +525,14 @@ const Kernel kDirect[] = {
     {run_thin<1, 1, 4>, 16, 16, 256, 4, 256, false, 2.22f, 0.683f, 0.f, 0.775f},
 };
 const Kernel kAny[] = {
-    {run_tile<Shape<false, 128, 256, 2, 4, 2>>, 128, 256, 128, 1, kAll, true, 0.f, 0.f, 6.57f, 1.32f},
-    {run_tile<Shape<false, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, kAll, true, 0.f, 0.f, 4.38f, 0.872f},
-    {run_tile<Shape<false, 128, 64, 4, 2, 2>>, 128, 64, 128, 1, kAll, true, 0.f, 0.f, 3.67f, 0.621f},
-    {run_tile<Shape<false, 64, 64, 2, 4, 2>>, 64, 64, 128, 1, kAll, true, 1.79f, 0.485f, 1.32f, 0.432f},
-    {run_tile<Shape<false, 32, 64, 1, 4, 2, 2>>, 32, 64, 128, 2, kAll, true, 1.51f, 0.f, 1.82f, 0.702f},
-    {run_tile<Shape<false, 32, 32, 2, 2, 2, 2>>, 32, 32, 128, 2, kAll, true, 2.17f, 0.508f, 0.662f, 0.403f},
-    {run_tile<Shape<false, 32, 32, 2, 2, 2, 4>>, 32, 32, 128, 4, kAll, true, 1.6f, 0.f, 1.06f, 0.794f},
-    {run_thin<1, 1, 4>, 16, 16, 256, 4, 64, true, 1.23f, 0.f, 0.f, 1.79f},
+    {run_tile<Shape<false, 128, 256, 2, 4, 2>>, 128, 256, 128, 1, kAll, true, 0.f, 0.f, 6.38f, 1.29f},
+    {run_tile<Shape<false, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, kAll, true, 0.f, 0.f, 4.32f, 0.78f},
+    {run_tile<Shape<false, 128, 64, 4, 2, 2>>, 128, 64, 128, 1, kAll, true, 0.231f, 0.f, 3.27f, 0.597f},
+    {run_tile<Shape<false, 64, 64, 2, 4, 2>>, 64, 64, 128, 1, kAll, true, 2.07f, 0.466f, 1.25f, 0.461f},
+    {run_tile<Shape<false, 32, 64, 1, 4, 2, 2>>, 32, 64, 128, 2, kAll, true, 2.52f, 0.00958f, 1.04f, 0.569f},
+    {run_tile<Shape<false, 32, 32, 2, 2, 2, 2>>, 32, 32, 128, 2, kAll, true, 2.4f, 0.545f, 0.501f, 0.363f},
+    {run_tile<Shape<false, 32, 32, 2, 2, 2, 4>>, 32, 32, 128, 4, kAll, true, 1.51f, 0.864f, 1.59f, 0.678f},
+    {run_thin<1, 1, 4>, 16, 16, 256, 4, 64, true, 0.993f, 2.07f, 0.f, 1.74f},
 };
 
 int run_product(const Product &p, hipStream_t stream)

@@ -365,7 +365,7 @@ LARGE_GROUPS = [
     ([100, 3, 300, 80], 9, 560, 416, "bf16"), ([40, 0, 90, 2], 4, 1980, 528, "f32"), ([200, 180, 200], 7, 560, 1104, "f16"), ([20, 0, 1, 40], 5, 300, 1040, "bf16"),
     ([300, 250], 20, 500, 784, "f32"), ([900, 0, 411, 500], 77, 1300, 501, "bf16"), ([300, 0, 900, 200], 20, 1300, 270, "f32"), ([150, 60, 200], 9, 700, 333, "f16"),
     ([410, 200, 0], 5, 573, 145, "f32"), ([20, 1, 0, 14], 2, 100, 275, "bf16"), ([100, 48], 9, 70, 900, "f32"), ([30, 1, 0, 9], 6, 60, 815, "bf16"),
-    ([700, 0, 333, 41, 690], 22, 578, 1387, "f16"), ([500, 533, 0], 10, 365, 2361, "bf16"), ([121, 12], 5, 40, 543, "f32"), ([1541, 2101], 10, 1049, 305, "f16"),
+    ([700, 0, 333, 41, 690], 22, 578, 1387, "f16"), ([500, 533, 0], 10, 365, 2361, "bf16"), ([121, 12], 5, 40, 543, "f32"), ([1541, 2101], 10, 1049, 305, "f16"), ([399, 203], 7, 776, 313, "f32"),
 ]
 
 
