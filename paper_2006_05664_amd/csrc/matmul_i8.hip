@@ -10,6 +10,7 @@
 
 #include "kernel.hpp"
 #include "narrow.hpp"
+#include "wave.hpp"
 
 namespace {
 
@@ -117,7 +118,7 @@ __device__ __forceinline__ void store_tile(const Product &p, const Rows &r, int 
             const int piece = j * 4 + (lane >> 4), chunk = (piece / OF) ^ (lane & 15) % CPR;     // a row's chunks are permuted, so that 16 rows fall on different banks
             __builtin_memcpy(__builtin_assume_aligned(patch + (lane & 15) * PITCH + chunk * 16 + piece % OF * (16 / OF), 4 * sizeof(T)), v, sizeof v);
         }
-        __builtin_amdgcn_wave_barrier();
+        exchange();
         const long row0 = r.first + m0 + i * 16;
 #pragma unroll
         for (int u = 0; u < (16 * CPR + 63) / 64; ++u) {
@@ -131,7 +132,7 @@ __device__ __forceinline__ void store_tile(const Product &p, const Rows &r, int 
 #pragma unroll 1
                 for (int e = 0; e < cols - c; ++e) dst[e] = ((const T *)from)[e];
         }
-        __builtin_amdgcn_wave_barrier();
+        exchange();
     }
 }
 

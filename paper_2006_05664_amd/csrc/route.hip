@@ -11,6 +11,7 @@
 
 #include "kernel.hpp"
 #include "narrow.hpp"
+#include "wave.hpp"
 
 namespace {
 
@@ -102,7 +103,7 @@ __device__ __forceinline__ void route_rows(const Route &r, long first_slot, int 
             const bool valid = (unsigned)e < (unsigned)r.experts;
             const int key = valid ? e * 64 + tid : INT32_MAX;
             s.total[tid] = key;
-            __builtin_amdgcn_wave_barrier();
+            exchange();
             auto smaller = [&](int than) {
                 int n = 0;
                 for (int i = 0; i < slots; i += 4)          // one wave, whose LDS accesses keep their order
@@ -177,7 +178,7 @@ __device__ __forceinline__ void route_rows(const Route &r, long first_slot, int 
             s.held = run;
             if (writes) r.offsets[r.experts] = run;
         }
-        __builtin_amdgcn_wave_barrier();
+        exchange();
         int earlier = 0;
         for (int i = 0; i < own; ++i) {
             const int other = __builtin_amdgcn_readlane(slot, i);
