@@ -8,7 +8,7 @@
 #include <algorithm>
 #include <cstdint>
 
-#include "kernel.hpp"
+#include "launch.hpp"
 #include "narrow.hpp"
 #include "wave.hpp"
 
@@ -488,17 +488,13 @@ dim3 grid_of(const Product &p, int bm, int bn)
 template <typename S>
 int run_tile(const Product &p, hipStream_t stream)
 {
-    hipLaunchKernelGGL(product_tile<S>, grid_of(p, S::BM, S::BN), dim3(S::NT), 0, stream, p);
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? OPEVO_OK : opevo::hip_fail(e, "product launch");
+    return opevo::launch("product launch", product_tile<S>, grid_of(p, S::BM, S::BN), dim3(S::NT), stream, p);
 }
 
 template <int MI, int NI, int W>
 int run_thin(const Product &p, hipStream_t stream)
 {
-    hipLaunchKernelGGL((product_thin<MI, NI, W>), grid_of(p, MI * 16, NI * 16), dim3(W * 64), 0, stream, p);
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? OPEVO_OK : opevo::hip_fail(e, "product launch");
+    return opevo::launch("product launch", (product_thin<MI, NI, W>), grid_of(p, MI * 16, NI * 16), dim3(W * 64), stream, p);
 }
 
 // A kernel and what it takes, in us: launch + max(steps * chain, load * (tile + steps * rate)), where steps is how many slabs (thin: steps of 256 values) a wave

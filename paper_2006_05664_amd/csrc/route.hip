@@ -9,7 +9,7 @@
 #include <algorithm>
 #include <cstdint>
 
-#include "kernel.hpp"
+#include "launch.hpp"
 #include "narrow.hpp"
 #include "wave.hpp"
 
@@ -527,16 +527,11 @@ void route_combine_grad(const T *__restrict__ dy, long ld_dy, const T *__restric
 
 // ------------------------------------------------------------------ host side
 using opevo::fail;
+using opevo::launch;
 
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 size_t size_of(int dtype) { return dtype == OPEVO_F32 ? 4 : 2; }
 bool known(int dtype) { return dtype == OPEVO_F32 || dtype == OPEVO_BF16 || dtype == OPEVO_F16; }
-
-int launched(const char *what)
-{
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? OPEVO_OK : opevo::hip_fail(e, what);
-}
 
 int check_route(const char *who, int64_t tokens, int k, int experts)
 {
@@ -583,8 +578,7 @@ int plan_route(const char *who, const int32_t *expert, int64_t tokens, int k, in
         const size_t need = sizeof(int) * (size_t)r->chunks * experts;
         if (!workspace || !aligned(workspace, 4) || workspace_bytes < need)
             return fail(OPEVO_E_ARG, "%s: the workspace holds %zu bytes of the %zu it takes, or is not aligned to 4 bytes", who, workspace ? workspace_bytes : 0, need);
-        hipLaunchKernelGGL(route_count, dim3(r->chunks), dim3(kThreads), 0, stream, expert, (long)slots, r->chunk, experts, static_cast<int *>(workspace));
-        if (int rc = launched("route_count launch")) return rc;
+        if (int rc = launch("route_count launch", route_count, dim3(r->chunks), dim3(kThreads), stream, expert, (long)slots, r->chunk, experts, static_cast<int *>(workspace))) return rc;
         r->counts = static_cast<const int *>(workspace);
     }
     return OPEVO_OK;
@@ -606,9 +600,8 @@ int run_dispatch(Route r, const void *x, int64_t ld_x, int64_t width, void *rows
     const int64_t blocks = std::max<int64_t>(1, (r.tokens + r.tokens_per_block - 1) / r.tokens_per_block);
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((pieces + l.tx * l.hold - 1) / (l.tx * l.hold), 512 / blocks));
     auto *k = width < Vec<T>::n ? route_dispatch<T, 1, false> : l.hold == 1 ? route_dispatch<T, 1, true> : l.hold == 2 ? route_dispatch<T, 2, true> : route_dispatch<T, 4, true>;
-    hipLaunchKernelGGL(k, dim3((unsigned)blocks, (unsigned)parts), dim3(kThreads), 0, stream, r, static_cast<const T *>(x), (long)ld_x,
+    return launch("route_dispatch launch", k, dim3((unsigned)blocks, (unsigned)parts), dim3(kThreads), stream, r, static_cast<const T *>(x), (long)ld_x,
                        (int)width, l.tx, static_cast<T *>(rows), (long)ld_rows);
-    return launched("route_dispatch launch");
 }
 template <typename T>
 int run_dispatch_i8(Route r, const void *x, int64_t ld_x, int64_t width, int8_t *q, int64_t ld_q, float *scale, hipStream_t stream)
@@ -617,9 +610,8 @@ int run_dispatch_i8(Route r, const void *x, int64_t ld_x, int64_t width, int8_t 
     deal(&r, l.ty);
     const int64_t blocks = std::max<int64_t>(1, (r.tokens + r.tokens_per_block - 1) / r.tokens_per_block);
     auto *k = width < Vec<T>::n ? route_dispatch_i8<T, 1, false> : l.hold == 1 ? route_dispatch_i8<T, 1, true> : l.hold == 2 ? route_dispatch_i8<T, 2, true> : route_dispatch_i8<T, 4, true>;
-    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kThreads), 0, stream, r, static_cast<const T *>(x), (long)ld_x, (int)width, l.tx,
+    return launch("route_dispatch_i8 launch", k, dim3((unsigned)blocks), dim3(kThreads), stream, r, static_cast<const T *>(x), (long)ld_x, (int)width, l.tx,
                        q, (long)ld_q, scale);
-    return launched("route_dispatch_i8 launch");
 }
 template <typename T>
 int run_quantize(const void *x, int64_t ld_x, int64_t rows, int64_t width, int8_t *q, int64_t ld_q, float *scale, hipStream_t stream)
@@ -627,9 +619,8 @@ int run_quantize(const void *x, int64_t ld_x, int64_t rows, int64_t width, int8_
     const Lay l = lay_out((width + Vec<T>::n - 1) / Vec<T>::n, rows, 4);
     const int64_t blocks = (rows + l.ty - 1) / l.ty;
     auto *k = width < Vec<T>::n ? quantize_rows<T, 1, false> : l.hold == 1 ? quantize_rows<T, 1, true> : l.hold == 2 ? quantize_rows<T, 2, true> : quantize_rows<T, 4, true>;
-    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(kThreads), 0, stream, static_cast<const T *>(x), (long)ld_x, (long)rows, (int)width, l.tx,
+    return launch("quantize_rows launch", k, dim3((unsigned)blocks), dim3(kThreads), stream, static_cast<const T *>(x), (long)ld_x, (long)rows, (int)width, l.tx,
                        q, (long)ld_q, scale);
-    return launched("quantize_rows launch");
 }
 template <typename T>
 int run_combine(const void *rows, int64_t ld_rows, const float *weight, const int32_t *row_of_slot, int64_t tokens, int k, int64_t width, void *y,
@@ -640,9 +631,8 @@ int run_combine(const void *rows, int64_t ld_rows, const float *weight, const in
     const int64_t blocks = (tokens + l.ty - 1) / l.ty;
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((pieces + l.tx - 1) / l.tx, 1024 / blocks));
     auto *kernel = width < Vec<T>::n ? route_combine<T, false> : route_combine<T, true>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, (unsigned)parts), dim3(kThreads), 0, stream, static_cast<const T *>(rows), (long)ld_rows, weight,
+    return launch("route_combine launch", kernel, dim3((unsigned)blocks, (unsigned)parts), dim3(kThreads), stream, static_cast<const T *>(rows), (long)ld_rows, weight,
                        row_of_slot, (long)tokens, k, (int)width, l.tx, static_cast<T *>(y), (long)ld_y);
-    return launched("route_combine launch");
 }
 template <typename T>
 int run_combine_grad(const void *dy, int64_t ld_dy, const void *rows, int64_t ld_rows, const float *weight, const int32_t *row_of_slot, const int32_t *held_at,
@@ -654,10 +644,9 @@ int run_combine_grad(const void *dy, int64_t ld_dy, const void *rows, int64_t ld
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(k, 2048 / blocks));
     const int share = (int)((k + parts - 1) / parts);
     auto *kernel = width < Vec<T>::n ? route_combine_grad<T, false> : route_combine_grad<T, true>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, (unsigned)((k + share - 1) / share)), dim3(kThreads), 0, stream, static_cast<const T *>(dy), (long)ld_dy,
+    return launch("route_combine_grad launch", kernel, dim3((unsigned)blocks, (unsigned)((k + share - 1) / share)), dim3(kThreads), stream, static_cast<const T *>(dy), (long)ld_dy,
                        static_cast<const T *>(rows), (long)ld_rows, weight, row_of_slot, held_at, (long)tokens, k, (int)width, l.tx, share, static_cast<T *>(drows),
                        (long)ld_drows, dweight);
-    return launched("route_combine_grad launch");
 }
 
 }  // namespace
