@@ -74,6 +74,35 @@ void route_count(const int *__restrict__ expert, long slots, int chunk, int expe
     for (int e = threadIdx.x; e < experts; e += kThreads) counts[(long)blockIdx.x * experts + e] = hist[e];
 }
 
+// The counts of a chunk become those of all chunks before it, and behind the last chunk come those of all: a workgroup of the dispatch reads two lines of them instead of all
+// lines, which would make the sort's work grow with the square of the slots.  A workgroup takes kScanCols experts; each of its lines of lanes takes as many chunks as the others,
+// adds them up, and goes through them again from the sum of the lines before it.
+constexpr int kScanCols = 16, kScanThreads = 1024, kScanLines = kScanThreads / kScanCols;
+__global__ __launch_bounds__(kScanThreads)
+void route_scan(int *counts, int chunks, int experts)
+{
+    __shared__ int sums[kScanLines][kScanCols];
+    const int col = (int)threadIdx.x % kScanCols, line = (int)threadIdx.x / kScanCols, e = blockIdx.x * kScanCols + col;
+    const int share = (chunks + kScanLines - 1) / kScanLines, first = min(line * share, chunks), last = min(first + share, chunks);
+    const bool on = e < experts;
+    int sum = 0;
+    if (on)
+#pragma unroll 8
+        for (int c = first; c < last; ++c) sum += counts[(long)c * experts + e];
+    sums[line][col] = sum;
+    __syncthreads();
+    if (!on) return;
+    int run = 0;
+    for (int l = 0; l < line; ++l) run += sums[l][col];
+#pragma unroll 8
+    for (int c = first; c < last; ++c) {
+        const int n = counts[(long)c * experts + e];
+        counts[(long)c * experts + e] = run;
+        run += n;
+    }
+    if (line == kScanLines - 1) counts[(long)chunks * experts + e] = run;
+}
+
 constexpr int kFew = 16;                // slots that one wave sorts by comparing them
 constexpr int kOwn = 64;                // slots of a workgroup at most: one wave ranks them
 
@@ -83,13 +112,14 @@ struct Route {
     int k, experts;
     const int *counts;      // NULL: every workgroup counts all slots itself
     int chunk, chunks;
+    bool scanned;           // counts[c] are those of the chunks before c, c up to `chunks`
     int tokens_per_block;
     int *offsets, *row_of_slot;
 };
 struct Sorted { __attribute__((aligned(16))) int total[kMaxExperts]; int before[kMaxExperts], place[kOwn], held; };
 
 // Rows of this workgroup's slots into place[] (-1: none), from the slots' experts alone: a slot's row is the number of slots of
-// lower experts, plus the earlier slots of its own.  Earlier slots are those of earlier chunks (counted by route_count, a column sum), those of
+// lower experts, plus the earlier slots of its own.  Earlier slots are those of earlier chunks (counted by route_count; a column sum, which route_scan has made of it where there are many), those of
 // its chunk before this workgroup's first (counted here), and those of this workgroup before it.  Integer counts: any order gives the same.
 // held: the number of slots that have a row.
 __device__ __forceinline__ void route_rows(const Route &r, long first_slot, int own, Sorted &s, bool writes)
@@ -125,8 +155,13 @@ __device__ __forceinline__ void route_rows(const Route &r, long first_slot, int 
     __syncthreads();
     if (r.counts) {
         const int at = (int)(first_slot >> __builtin_ctz(r.chunk));     // chunks are powers of two
+        if (r.scanned)
+            for (int e = tid; e < r.experts; e += kThreads) {
+                s.total[e] = r.counts[(long)r.chunks * r.experts + e];
+                atomicAdd(&s.before[e], r.counts[(long)at * r.experts + e]);
+            }
         const int lines = kThreads / r.experts > 1 ? kThreads / r.experts : 1, line = lines > 1 ? tid / r.experts : 0;
-        for (int e = lines > 1 ? tid - line * r.experts : tid; e < r.experts && line < lines; e += kThreads) {
+        for (int e = lines > 1 ? tid - line * r.experts : tid; !r.scanned && e < r.experts && line < lines; e += kThreads) {
             int total = 0, before = 0;
 #pragma unroll 16
             for (int c = line; c < r.chunks; c += lines) {
@@ -564,21 +599,35 @@ int64_t chunk_of(int64_t slots, int experts)
     return chunk;
 }
 
-// Fills r and, where it takes one, launches the count.
+// Whether a third kernel adds the counts up along the chunks, or every workgroup (at most kOwn slots) does for itself: by the counts that all of them together would read.  Rows
+// of 64 bf16, us without / with the scan: 131072 slots of 128 experts (64 chunks) 21.6 / 20.7, 32768 of 1024 (16) 17.8 / 18.9, 131072 of 1024 (32) 41.8 / 33.8, 2^20 of 256 (128)
+// 186 / 115, 2^23 of 256 (1024) 7250 / 880; rows of 2048, 2^20 slots of 256 experts 984 / 982.
+bool scans(int64_t slots, int64_t chunks, int experts) { return slots * chunks * experts > (int64_t)1 << 30; }
+size_t workspace_of(int64_t slots, int experts)
+{
+    if (slots <= kCountAlone) return 0;
+    const int64_t chunk = chunk_of(slots, experts), chunks = (slots + chunk - 1) / chunk;
+    return sizeof(int) * (size_t)(chunks + scans(slots, chunks, experts)) * experts;
+}
+
+// Fills r and, where it takes them, launches the count and the scan.
 int plan_route(const char *who, const int32_t *expert, int64_t tokens, int k, int experts, int32_t *offsets, int32_t *row_of_slot,
                void *workspace, size_t workspace_bytes, hipStream_t stream, Route *r)
 {
     const int64_t slots = tokens * k;
     r->expert = expert; r->tokens = tokens; r->k = k; r->experts = experts;
-    r->counts = nullptr; r->chunk = 1; r->chunks = 0;
+    r->counts = nullptr; r->chunk = 1; r->chunks = 0; r->scanned = false;
     r->offsets = offsets; r->row_of_slot = row_of_slot;
     if (slots > kCountAlone) {
         r->chunk = (int)chunk_of(slots, experts);
         r->chunks = (int)((slots + r->chunk - 1) / r->chunk);
-        const size_t need = sizeof(int) * (size_t)r->chunks * experts;
+        r->scanned = scans(slots, r->chunks, experts);
+        const size_t need = workspace_of(slots, experts);
         if (!workspace || !aligned(workspace, 4) || workspace_bytes < need)
             return fail(OPEVO_E_ARG, "%s: the workspace holds %zu bytes of the %zu it takes, or is not aligned to 4 bytes", who, workspace ? workspace_bytes : 0, need);
         if (int rc = launch("route_count launch", route_count, dim3(r->chunks), dim3(kThreads), stream, expert, (long)slots, r->chunk, experts, static_cast<int *>(workspace))) return rc;
+        if (r->scanned)
+            if (int rc = launch("route_scan launch", route_scan, dim3((experts + kScanCols - 1) / kScanCols), dim3(kScanThreads), stream, static_cast<int *>(workspace), r->chunks, experts)) return rc;
         r->counts = static_cast<const int *>(workspace);
     }
     return OPEVO_OK;
@@ -659,8 +708,7 @@ extern "C" int opevo_route_workspace(int64_t tokens, int k, int experts, size_t 
 {
     if (!bytes) return fail(OPEVO_E_ARG, "route_workspace: bytes is NULL");
     if (int rc = check_route("route_workspace", tokens, k, experts)) return rc;
-    const int64_t slots = tokens * k, chunk = chunk_of(slots, experts);
-    *bytes = slots > kCountAlone ? sizeof(int) * (size_t)((slots + chunk - 1) / chunk) * experts : 0;
+    *bytes = workspace_of(tokens * k, experts);
     return OPEVO_OK;
 }
 
