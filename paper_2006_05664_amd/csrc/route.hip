@@ -18,6 +18,14 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxExperts = OPEVO_ROUTE_MAX_EXPERTS;
 
+// A launch has fewer than 2^32 threads along an extent of its grid: workgroups go on in the third.
+constexpr int kGridX = 1 << 23;
+__device__ __forceinline__ long this_block() { return (long)blockIdx.z * kGridX + blockIdx.x; }
+dim3 spread(int64_t blocks, int64_t parts = 1)
+{
+    return dim3((unsigned)std::min<int64_t>(blocks, kGridX), (unsigned)parts, (unsigned)((blocks + kGridX - 1) / kGridX));
+}
+
 // A row is taken in pieces of 16 bytes.  Rows start wherever the caller's row length puts them, so all accesses are made for any alignment (the hardware's
 // 16-byte loads and stores take any address; the compiler is told nothing more).  Where the width is no multiple of a piece, the last piece ends with the row and overlaps the
 // one before it: both write the same values.  A row shorter than a piece is one, taken element by element.
@@ -114,6 +122,7 @@ struct Route {
     int chunk, chunks;
     bool scanned;           // counts[c] are those of the chunks before c, c up to `chunks`
     int tokens_per_block;
+    long blocks;
     int *offsets, *row_of_slot;
 };
 struct Sorted { __attribute__((aligned(16))) int total[kMaxExperts]; int before[kMaxExperts], place[kOwn], held; };
@@ -247,7 +256,8 @@ __global__ __launch_bounds__(kThreads)
 void route_dispatch(Route r, const T *__restrict__ x, long ld_x, int width, int tx, T *__restrict__ rows, long ld_rows)
 {
     __shared__ Sorted s;
-    const long first = (long)blockIdx.x * r.tokens_per_block;
+    const long block = this_block(), first = block * r.tokens_per_block;
+    if (first >= r.tokens && block > 0) return;
     const int tokens = (int)(r.tokens - first < r.tokens_per_block ? r.tokens - first : r.tokens_per_block), own = tokens * r.k;
     const Pieces<T, WIDE> at(width);
     const int lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx), line = (int)threadIdx.x >> __builtin_ctz(tx);
@@ -260,7 +270,7 @@ void route_dispatch(Route r, const T *__restrict__ x, long ld_x, int width, int 
     };
     int t = line, c = start;
     load(v, t, c);
-    route_rows(r, first * r.k, own, s, blockIdx.x == 0 && blockIdx.y == 0);
+    route_rows(r, first * r.k, own, s, block == 0 && blockIdx.y == 0);
     if (blockIdx.y == 0 && (int)threadIdx.x < own) r.row_of_slot[first * r.k + threadIdx.x] = s.place[threadIdx.x];
     while (t < tokens) {
         int next_t = t, next_c = c + step;
@@ -279,7 +289,7 @@ void route_dispatch(Route r, const T *__restrict__ x, long ld_x, int width, int 
     }
     // rows that no slot goes to
     const Vec<T> zero = {};
-    for (long row = s.held + (long)blockIdx.x * ty + line; row < r.tokens * r.k; row += (long)gridDim.x * ty)
+    for (long row = s.held + block * ty + line; row < r.tokens * r.k; row += r.blocks * ty)
         for (int i = blockIdx.y * tx + lane; i < at.count; i += tx * gridDim.y) at.store(rows + row * ld_rows, i, zero.v);
 }
 
@@ -396,7 +406,7 @@ void quantize_rows(const T *__restrict__ x, long ld_x, long rows, int width, int
 {
     __shared__ unsigned red[kThreads / 64];
     const int lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx);
-    const long row = (long)blockIdx.x * ty + ((int)threadIdx.x >> __builtin_ctz(tx));
+    const long row = this_block() * ty + ((int)threadIdx.x >> __builtin_ctz(tx));
     const bool on = row < rows;
     const T *src = x + (on ? row : 0) * ld_x;
     const Pieces<T, WIDE> at(width);
@@ -420,13 +430,14 @@ void route_dispatch_i8(Route r, const T *__restrict__ x, long ld_x, int width, i
 {
     __shared__ Sorted s;
     __shared__ unsigned red[kThreads / 64];
-    const long first = (long)blockIdx.x * r.tokens_per_block;
+    const long block = this_block(), first = block * r.tokens_per_block;
+    if (first >= r.tokens && block > 0) return;
     const int tokens = (int)(r.tokens - first < r.tokens_per_block ? r.tokens - first : r.tokens_per_block), own = tokens * r.k;
     const int lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx), line = (int)threadIdx.x >> __builtin_ctz(tx);
     const Pieces<T, WIDE> at(width);
     Held<T, kHold, WIDE> h, next;
     h.load(at, x + (first + line) * ld_x, lane, tx, line < tokens);
-    route_rows(r, first * r.k, own, s, blockIdx.x == 0);
+    route_rows(r, first * r.k, own, s, block == 0);
     if ((int)threadIdx.x < own) r.row_of_slot[first * r.k + threadIdx.x] = s.place[threadIdx.x];
     for (int t0 = 0; t0 < tokens; t0 += ty) {               // alike for all threads: row_max is for all together
         const int t = t0 + line;
@@ -453,7 +464,7 @@ void route_dispatch_i8(Route r, const T *__restrict__ x, long ld_x, int width, i
         h = next;
     }
     const int8_t zero[Vec<T>::n] = {};
-    for (long row = s.held + (long)blockIdx.x * ty + line; row < r.tokens * r.k; row += (long)gridDim.x * ty) {
+    for (long row = s.held + block * ty + line; row < r.tokens * r.k; row += r.blocks * ty) {
         for (int i = lane; i < at.count; i += tx) at.store(q + row * ld_q, i, zero);
         if (lane == 0) scale[row] = 0.f;
     }
@@ -470,7 +481,7 @@ void route_combine(const T *__restrict__ rows, long ld_rows, const float *__rest
                    long tokens, int k, int width, int tx, T *__restrict__ y, long ld_y)
 {
     const int lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx);
-    const long t = (long)blockIdx.x * ty + ((int)threadIdx.x >> __builtin_ctz(tx)), slots = tokens * k;
+    const long t = this_block() * ty + ((int)threadIdx.x >> __builtin_ctz(tx)), slots = tokens * k;
     if (t >= tokens) return;
     const Pieces<T, WIDE> at(width);
     for (int i = blockIdx.y * tx + lane; i < at.count; i += tx * gridDim.y) {
@@ -516,7 +527,7 @@ void route_combine_grad(const T *__restrict__ dy, long ld_dy, const T *__restric
     __shared__ float red[OPEVO_ROUTE_MAX_SLOTS][kThreads / 64];
     const int j0 = blockIdx.y * share, j1 = min(k, j0 + share);
     const int lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx), line = (int)threadIdx.x >> __builtin_ctz(tx);
-    const long t = (long)blockIdx.x * ty + line, slots = tokens * k;
+    const long t = this_block() * ty + line, slots = tokens * k;
     const bool on = t < tokens;
     const Pieces<T, WIDE> at(width);
     for (int j = j0; j < j1; ++j) {
@@ -556,7 +567,7 @@ void route_combine_grad(const T *__restrict__ dy, long ld_dy, const T *__restric
     }
     const Vec<T> zero = {};
     const int held = *held_at;
-    for (long row = (held > 0 ? held : 0) + ((long)blockIdx.y * gridDim.x + blockIdx.x) * ty + line; row < slots; row += (long)gridDim.y * gridDim.x * ty)
+    for (long row = (held > 0 ? held : 0) + ((long)blockIdx.y * gridDim.x * gridDim.z + this_block()) * ty + line; row < slots; row += (long)gridDim.y * gridDim.x * gridDim.z * ty)
         for (int i = lane; i < at.count; i += tx) at.store(drows + row * ld_drows, i, zero.v);
 }
 
@@ -638,6 +649,7 @@ void deal(Route *r, int ty)
 {
     const int64_t most = kOwn / r->k, share = r->tokens / (r->counts ? 1024 : 256);
     r->tokens_per_block = (int)std::max<int64_t>(1, std::min(std::max<int64_t>(ty, share / ty * ty), most));
+    r->blocks = std::max<int64_t>(1, (r->tokens + r->tokens_per_block - 1) / r->tokens_per_block);
 }
 
 template <typename T>
@@ -646,10 +658,9 @@ int run_dispatch(Route r, const void *x, int64_t ld_x, int64_t width, void *rows
     const int64_t pieces = (width + Vec<T>::n - 1) / Vec<T>::n;
     const Lay l = lay_out(pieces, r.tokens, 4);
     deal(&r, l.ty);
-    const int64_t blocks = std::max<int64_t>(1, (r.tokens + r.tokens_per_block - 1) / r.tokens_per_block);
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((pieces + l.tx * l.hold - 1) / (l.tx * l.hold), 512 / blocks));
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((pieces + l.tx * l.hold - 1) / (l.tx * l.hold), 512 / r.blocks));
     auto *k = width < Vec<T>::n ? route_dispatch<T, 1, false> : l.hold == 1 ? route_dispatch<T, 1, true> : l.hold == 2 ? route_dispatch<T, 2, true> : route_dispatch<T, 4, true>;
-    return launch("route_dispatch launch", k, dim3((unsigned)blocks, (unsigned)parts), dim3(kThreads), stream, r, static_cast<const T *>(x), (long)ld_x,
+    return launch("route_dispatch launch", k, spread(r.blocks, parts), dim3(kThreads), stream, r, static_cast<const T *>(x), (long)ld_x,
                        (int)width, l.tx, static_cast<T *>(rows), (long)ld_rows);
 }
 template <typename T>
@@ -657,9 +668,8 @@ int run_dispatch_i8(Route r, const void *x, int64_t ld_x, int64_t width, int8_t 
 {
     const Lay l = lay_out((width + Vec<T>::n - 1) / Vec<T>::n, r.tokens, 4);
     deal(&r, l.ty);
-    const int64_t blocks = std::max<int64_t>(1, (r.tokens + r.tokens_per_block - 1) / r.tokens_per_block);
     auto *k = width < Vec<T>::n ? route_dispatch_i8<T, 1, false> : l.hold == 1 ? route_dispatch_i8<T, 1, true> : l.hold == 2 ? route_dispatch_i8<T, 2, true> : route_dispatch_i8<T, 4, true>;
-    return launch("route_dispatch_i8 launch", k, dim3((unsigned)blocks), dim3(kThreads), stream, r, static_cast<const T *>(x), (long)ld_x, (int)width, l.tx,
+    return launch("route_dispatch_i8 launch", k, spread(r.blocks), dim3(kThreads), stream, r, static_cast<const T *>(x), (long)ld_x, (int)width, l.tx,
                        q, (long)ld_q, scale);
 }
 template <typename T>
@@ -668,7 +678,7 @@ int run_quantize(const void *x, int64_t ld_x, int64_t rows, int64_t width, int8_
     const Lay l = lay_out((width + Vec<T>::n - 1) / Vec<T>::n, rows, 4);
     const int64_t blocks = (rows + l.ty - 1) / l.ty;
     auto *k = width < Vec<T>::n ? quantize_rows<T, 1, false> : l.hold == 1 ? quantize_rows<T, 1, true> : l.hold == 2 ? quantize_rows<T, 2, true> : quantize_rows<T, 4, true>;
-    return launch("quantize_rows launch", k, dim3((unsigned)blocks), dim3(kThreads), stream, static_cast<const T *>(x), (long)ld_x, (long)rows, (int)width, l.tx,
+    return launch("quantize_rows launch", k, spread(blocks), dim3(kThreads), stream, static_cast<const T *>(x), (long)ld_x, (long)rows, (int)width, l.tx,
                        q, (long)ld_q, scale);
 }
 template <typename T>
@@ -680,7 +690,7 @@ int run_combine(const void *rows, int64_t ld_rows, const float *weight, const in
     const int64_t blocks = (tokens + l.ty - 1) / l.ty;
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>((pieces + l.tx - 1) / l.tx, 1024 / blocks));
     auto *kernel = width < Vec<T>::n ? route_combine<T, false> : route_combine<T, true>;
-    return launch("route_combine launch", kernel, dim3((unsigned)blocks, (unsigned)parts), dim3(kThreads), stream, static_cast<const T *>(rows), (long)ld_rows, weight,
+    return launch("route_combine launch", kernel, spread(blocks, parts), dim3(kThreads), stream, static_cast<const T *>(rows), (long)ld_rows, weight,
                        row_of_slot, (long)tokens, k, (int)width, l.tx, static_cast<T *>(y), (long)ld_y);
 }
 template <typename T>
@@ -693,7 +703,7 @@ int run_combine_grad(const void *dy, int64_t ld_dy, const void *rows, int64_t ld
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(k, 2048 / blocks));
     const int share = (int)((k + parts - 1) / parts);
     auto *kernel = width < Vec<T>::n ? route_combine_grad<T, false> : route_combine_grad<T, true>;
-    return launch("route_combine_grad launch", kernel, dim3((unsigned)blocks, (unsigned)((k + share - 1) / share)), dim3(kThreads), stream, static_cast<const T *>(dy), (long)ld_dy,
+    return launch("route_combine_grad launch", kernel, spread(blocks, (k + share - 1) / share), dim3(kThreads), stream, static_cast<const T *>(dy), (long)ld_dy,
                        static_cast<const T *>(rows), (long)ld_rows, weight, row_of_slot, held_at, (long)tokens, k, (int)width, l.tx, share, static_cast<T *>(drows),
                        (long)ld_drows, dweight);
 }
