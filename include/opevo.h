@@ -506,8 +506,9 @@ int opevo_route_combine_grad(const void *dy, int64_t ld_dy, const void *rows, in
                              const int32_t *row_of_slot, const int32_t *offsets, int experts, int64_t tokens, int k, int64_t width,
                              void *drows, int64_t ld_drows, float *dweight, void *stream);
 /* Rows to 8 bits: with a = the largest magnitude of a row, scale = a / 127 and q = 127 x / a rounded to the nearest integer, ties to even
- * (for bf16 / fp16 the rounding of the exact quotient; for fp32 inputs that of a quotient right to 2^-24).  A row of zeros has q = 0 and
- * scale = 0; a row that holds an infinity or a NaN has q = 0 and scale = NaN, so that what is computed from it is NaN. */
+ * (for bf16 / fp16 the rounding of the exact quotient; for fp32 inputs that of a quotient right to 2^-23 of its value: 127 x and
+ * the division are rounded to fp32 each).  A row of zeros has q = 0 and scale = 0; a row that holds an infinity or a NaN has q = 0 and
+ * scale = NaN, so that what is computed from it is NaN. */
 int opevo_quantize_rows_i8(const void *x, int64_t ld_x, int dtype, int64_t rows, int64_t width, int8_t *q, int64_t ld_q,
                            float *scale, void *stream);
 /* C[m, n] = (sum over k of A[m, k] * B[n, k]) * (scale_a[m] * scale_b[n]), the sum exact in 32-bit integers, then rounded to fp32, multiplied, and rounded to

@@ -317,7 +317,8 @@ template <> __device__ __forceinline__ float value_of<float>(unsigned m) { retur
 
 // q = round(127 x / a), a the row's largest magnitude.  With 127 x computed first (exact for 16-bit inputs: 11 + 7 bits) and one
 // division, the quotient of two numbers of at most 18 and 11 bits is a tie in fp32 only where it is one exactly, so the result is the
-// rounding of the exact quotient; fp32 inputs may differ from it where the quotient is within 2^-24 of a tie.  8192 rows of 4096 bf16 take 25 us (4.0 TB/s).  A division takes ten instructions: x times 127 / a, off by at most
+// rounding of the exact quotient; of fp32 inputs 127 x is rounded too, and where the exact quotient is within 2^-23 of its value from a tie (1.52e-5 at
+// the most) the other integer may come out.  8192 rows of 4096 bf16 take 25 us (4.0 TB/s).  A division takes ten instructions: x times 127 / a, off by at most
 // 2.3e-5 from that, rounds to the same integer unless it is within 4e-5 of a tie, and only then are the piece's eight values divided.
 template <typename T> struct Quantizer {
     float a, pre, inv, scale;
