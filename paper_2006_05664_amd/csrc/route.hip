@@ -694,15 +694,19 @@ int run_combine(const void *rows, int64_t ld_rows, const float *weight, const in
     return launch("route_combine launch", kernel, spread(blocks, parts), dim3(kThreads), stream, static_cast<const T *>(rows), (long)ld_rows, weight,
                        row_of_slot, (long)tokens, k, (int)width, l.tx, static_cast<T *>(y), (long)ld_y);
 }
+// Few tokens: a token's slots, one trip to memory after another in one workgroup, are dealt to several (509 tokens of 1001 fp16, 8 slots: 12.8 us in one, 7.0 in eight).
+int slots_a_workgroup(int64_t blocks, int k)
+{
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(k, 2048 / blocks));
+    return (int)((k + parts - 1) / parts);
+}
 template <typename T>
 int run_combine_grad(const void *dy, int64_t ld_dy, const void *rows, int64_t ld_rows, const float *weight, const int32_t *row_of_slot, const int32_t *held_at,
                      int64_t tokens, int k, int64_t width, void *drows, int64_t ld_drows, float *dweight, hipStream_t stream)
 {
     const Lay l = lay_out((width + Vec<T>::n - 1) / Vec<T>::n, tokens, 1);
     const int64_t blocks = (tokens + l.ty - 1) / l.ty;
-    // few tokens: a token's slots, one trip to memory after another in one workgroup, are dealt to several (509 tokens of 1001 fp16, 8 slots: 12.8 us in one, 7.0 in eight)
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(k, 2048 / blocks));
-    const int share = (int)((k + parts - 1) / parts);
+    const int share = slots_a_workgroup(blocks, k);
     auto *kernel = width < Vec<T>::n ? route_combine_grad<T, false> : route_combine_grad<T, true>;
     return launch("route_combine_grad launch", kernel, spread(blocks, (k + share - 1) / share), dim3(kThreads), stream, static_cast<const T *>(dy), (long)ld_dy,
                        static_cast<const T *>(rows), (long)ld_rows, weight, row_of_slot, held_at, (long)tokens, k, (int)width, l.tx, share, static_cast<T *>(drows),
