@@ -25,6 +25,13 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+def _expect(name: str, t: torch.Tensor, shape, dtypes, device) -> None:
+    """The library is given pointers: what they point to has to be what it takes them for."""
+    if tuple(t.shape) != tuple(shape) or t.dtype not in dtypes or t.device != device or not t.is_contiguous():
+        raise ValueError("%s: %s of shape %s on %s%s, not contiguous %s of shape %s on %s" % (
+            name, t.dtype, tuple(t.shape), t.device, "" if t.is_contiguous() else ", strided", " / ".join(str(d) for d in dtypes), tuple(shape), device))
+
+
 def quantize(x: torch.Tensor):
     """Rows of a contiguous matrix in 8 bits and their scales."""
     rows, width = x.shape
@@ -39,11 +46,16 @@ class ExpertLayer:
     def __init__(self, up: torch.Tensor, down: torch.Tensor):
         self.experts, self.inner, self.width = up.shape
         self.up, self.down = up.contiguous(), down.contiguous()
+        _expect("up", self.up, self.up.shape, _CODE, self.up.device)
+        _expect("down", self.down, (self.experts, self.width, self.inner), (up.dtype,), up.device)
         self.up8, self.up_scale = quantize(self.up.reshape(-1, self.width))          # laid out once
         self.down8, self.down_scale = quantize(self.down.reshape(-1, self.inner))
 
-    def _routing(self, ids: torch.Tensor):
+    def _routing(self, x: torch.Tensor, ids: torch.Tensor, weight: torch.Tensor):
         tokens, k = ids.shape
+        _expect("x", x, (tokens, self.width), _CODE, self.up.device)
+        _expect("ids", ids, (tokens, k), (torch.int32,), self.up.device)
+        _expect("weight", weight, (tokens, k), (torch.float32,), self.up.device)
         size = P.opevo_route_workspace(tokens, k, self.experts)
         return (tokens, k, torch.empty(self.experts + 1, dtype=torch.int32, device=ids.device), torch.empty(tokens * k, dtype=torch.int32, device=ids.device),
                 torch.empty(max(size, 4), dtype=torch.uint8, device=ids.device), size)
@@ -62,7 +74,7 @@ class ExpertLayer:
 
     def serve(self, x: torch.Tensor, ids: torch.Tensor, weight: torch.Tensor) -> torch.Tensor:
         """x [tokens, H], ids int32 [tokens, k] (an id outside [0, E): a slot held elsewhere), weight fp32 [tokens, k] -> [tokens, H]."""
-        tokens, k, offsets, row_of_slot, workspace, size = self._routing(ids)
+        tokens, k, offsets, row_of_slot, workspace, size = self._routing(x, ids, weight)
         rows = tokens * k
         q, scale = torch.empty(rows, self.width, dtype=torch.int8, device=x.device), torch.empty(rows, device=x.device)
         P.opevo_route_dispatch_i8(ids.data_ptr(), tokens, k, self.experts, x.data_ptr(), self.width, _CODE[x.dtype], self.width, offsets.data_ptr(),
@@ -74,7 +86,9 @@ class ExpertLayer:
 
     def train(self, x: torch.Tensor, ids: torch.Tensor, weight: torch.Tensor, dy: torch.Tensor):
         """(y, gradients of x, weight, up and down) for the gradient dy of y."""
-        tokens, k, offsets, row_of_slot, workspace, size = self._routing(ids)
+        _expect("x", x, x.shape, (self.up.dtype,), self.up.device)
+        _expect("dy", dy, x.shape, (x.dtype,), x.device)
+        tokens, k, offsets, row_of_slot, workspace, size = self._routing(x, ids, weight)
         rows = torch.empty(tokens * k, self.width, dtype=x.dtype, device=x.device)
         P.opevo_route_dispatch(ids.data_ptr(), tokens, k, self.experts, x.data_ptr(), self.width, _CODE[x.dtype], self.width, offsets.data_ptr(),
                                row_of_slot.data_ptr(), rows.data_ptr(), self.width, workspace.data_ptr(), size, _stream())
