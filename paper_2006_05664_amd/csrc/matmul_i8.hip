@@ -258,7 +258,8 @@ void product_thin(Product p)
 // Otherwise the slabs pass through registers, from where they start on any address: two stages in LDS, the slab after them on its way.
 // 8192^3: 256 x 256 tiles 416 - 433 us (2540 - 2640 TOP/s), matrix pipes 64 % busy; 386 with zero operands (power), 333 when all rows are the same (memory).  More stages of
 // shorter slabs 455, two workgroups of 256 x 128 a unit 525, 16 waves 732, 4 waves of 128 x 128 597, a workgroup that goes from tile to tile 426; through registers in
-// 128 x 256 tiles 552, and 4095^3, whose rows start anywhere, 114.  1000 x 1000 x 1008 in 64 x 64 tiles 5.7, 1000 x 1000 x 1001 7.7.
+// 128 x 256 tiles 552, and 4095^3, whose rows start anywhere, 114 (4096^3 60): 16 bytes from any address are 6.6 times as many
+// accesses of the L1 as 4096^3 makes, and the units that take the addresses apart are busy for 69 % of the time (40 %).  1000 x 1000 x 1008 in 64 x 64 tiles 5.7, 1000 x 1000 x 1001 7.7.
 template <bool DIRECT_, int BM_, int BN_, int WM_, int WN_, int STAGES_, int KG_ = 1>
 struct Shape {
     static constexpr bool DIRECT = DIRECT_;
@@ -501,7 +502,9 @@ int run_thin(const Product &p, hipStream_t stream)
 // goes through and load the workgroups for each of the 256 compute units, rounded up where that foretold the times better.  The first term is a workgroup's chain of latencies,
 // the second what a compute unit gets through.  The constants were fitted to the times of every kernel at 400 (rows apart by multiples of 16) and 450 (others)
 // random sizes of 1 - 8192 rows, 64 - 8192 columns and K of 64 - 8192; the kernel chosen by them took 0.8 % and 1.9 % more than the best of all of them in the
-// geometric mean, at most 1.5 times as much.
+// geometric mean, at most 1.5 times as much.  All of these were plain products.  By experts the same constants are used with the tiles that an even deal of the rows would make;
+// what a router deals makes more, and a ragged tile costs what a whole one does: 8192 rows over 8 experts, 34 - 37 tiles of 256 rows instead of 32, go in three rounds of
+// workgroups instead of two and take 58 us where the plain product of that size (N 4096, K 1024) takes 42.
 struct Kernel {
     int (*run)(const Product &, hipStream_t);
     int bm, bn, step, ways;             // tile, K of a step, waves or groups that share the steps

@@ -517,8 +517,9 @@ void route_combine(const T *__restrict__ rows, long ld_rows, const float *__rest
 }
 
 // drows[row_of_slot[s]] = w[s] dy[s / k], dw[s] = <dy[s / k], rows[row_of_slot[s]]>; rows from offsets[experts] on get zeros, slots without a row dw = 0.
-// Bound by memory: 8192 tokens of 4096 bf16 with four rows each move 604 MB.  One row is read and one written at a time by as many waves as fit: dy, which each slot reads
-// again, comes from the caches.  (All slots' rows at once, dy's pieces and the next row's held in registers: 140 - 180 us instead of 127 for that size.)
+// Bound by memory: 8192 tokens of 4096 bf16 with four rows each, 604 MB were each value moved once, take 118 us.  One row is read and one written at a time by as many waves as
+// fit.  dy, which each slot reads again, mostly comes from beyond the L2s again: 506 MB are read there instead of 336, 775 in all (6.6 TB/s, some of it from the memory's own
+// cache).  (All slots' rows at once, dy's pieces and the next row's held in registers: 140 - 180 us instead of 127 for that size.)
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(kThreads)
 void route_combine_grad(const T *__restrict__ dy, long ld_dy, const T *__restrict__ rows, long ld_rows, const float *__restrict__ weight,
@@ -601,7 +602,9 @@ int check_words(const char *who, const char *name, const void *p)
     return p && aligned(p, 4) ? OPEVO_OK : fail(OPEVO_E_ARG, "%s: %s is NULL or not aligned to 4 bytes", who, name);
 }
 
-// Up to this many slots every workgroup counts them all itself; beyond, route_count does it chunk by chunk.
+// Up to this many slots every workgroup counts them all itself; beyond, route_count does it chunk by chunk.  Rows of 1024 bf16, two slots a token, 8 / 64 / 256 experts, us by
+// themselves against counted: 2048 slots 4.8 / 4.7 / 5.7 against 6.7 / 6.9 / 9.3, 4096 6.9 / 6.9 / 7.9 against 8.0 / 8.5 / 10.4, 8192 10.6 / 10.7 / 11.6 against 9.6 / 11.6 / 11.4,
+// 16384 20.7 / 20.7 / 21.3 against 13.2 / 15.0 / 14.4.
 constexpr int64_t kCountAlone = 4096;
 // A workgroup reads chunks * experts counts and half a chunk of slots on average.
 int64_t chunk_of(int64_t slots, int experts)
@@ -611,7 +614,7 @@ int64_t chunk_of(int64_t slots, int experts)
     return chunk;
 }
 
-// Whether a third kernel adds the counts up along the chunks, or every workgroup (at most kOwn slots) does for itself: by the counts that all of them together would read.  Rows
+// Whether a third kernel adds the counts up along the chunks, or every workgroup (at most kOwn slots) does for itself: by what all of them together would read.  Rows
 // of 64 bf16, us without / with the scan: 131072 slots of 128 experts (64 chunks) 21.6 / 20.7, 32768 of 1024 (16) 17.8 / 18.9, 131072 of 1024 (32) 41.8 / 33.8, 2^20 of 256 (128)
 // 186 / 115, 2^23 of 256 (1024) 7250 / 880; rows of 2048, 2^20 slots of 256 experts 984 / 982.
 bool scans(int64_t slots, int64_t chunks, int experts) { return slots * chunks * experts > (int64_t)1 << 30; }
