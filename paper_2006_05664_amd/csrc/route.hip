@@ -11,6 +11,7 @@
 
 #include "launch.hpp"
 #include "narrow.hpp"
+#include "rows.hpp"
 #include "wave.hpp"
 
 namespace {
@@ -18,21 +19,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxExperts = OPEVO_ROUTE_MAX_EXPERTS;
 
-// A launch has fewer than 2^32 threads along an extent of its grid: workgroups go on in the third.
-constexpr int kGridX = 1 << 23;
-__device__ __forceinline__ long this_block() { return (long)blockIdx.z * kGridX + blockIdx.x; }
-dim3 spread(int64_t blocks, int64_t parts = 1)
-{
-    return dim3((unsigned)std::min<int64_t>(blocks, kGridX), (unsigned)parts, (unsigned)((blocks + kGridX - 1) / kGridX));
-}
-
 // A row is taken in pieces of 16 bytes.  Rows start wherever the caller's row length puts them, so all accesses are made for any alignment (the hardware's
 // 16-byte loads and stores take any address; the compiler is told nothing more).  Where the width is no multiple of a piece, the last piece ends with the row and overlaps the
 // one before it: both write the same values.  A row shorter than a piece is one, taken element by element.
-template <typename T> struct Vec {
-    static constexpr int n = 16 / sizeof(T);
-    T v[n];
-};
 template <typename T, bool WIDE> struct Pieces {     // WIDE: rows of at least a piece
     int width, count;
     __device__ explicit Pieces(int w) : width(w), count((w + Vec<T>::n - 1) / Vec<T>::n) {}
@@ -577,10 +566,6 @@ void route_combine_grad(const T *__restrict__ dy, long ld_dy, const T *__restric
 using opevo::fail;
 using opevo::launch;
 
-bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
-size_t size_of(int dtype) { return dtype == OPEVO_F32 ? 4 : 2; }
-bool known(int dtype) { return dtype == OPEVO_F32 || dtype == OPEVO_BF16 || dtype == OPEVO_F16; }
-
 int check_route(const char *who, int64_t tokens, int k, int experts)
 {
     if (tokens < 0 || k < 1 || k > OPEVO_ROUTE_MAX_SLOTS || tokens > INT32_MAX / k)
@@ -588,20 +573,6 @@ int check_route(const char *who, int64_t tokens, int k, int experts)
     if (experts < 1 || experts > kMaxExperts) return fail(OPEVO_E_ARG, "%s: %d experts (1 to %d)", who, experts, kMaxExperts);
     return OPEVO_OK;
 }
-// rows of `width` elements, `ld` apart
-int check_rows(const char *who, const char *name, const void *p, int64_t ld, int64_t width, size_t bytes)
-{
-    if (!p) return fail(OPEVO_E_ARG, "%s: %s is NULL", who, name);
-    if (!aligned(p, bytes)) return fail(OPEVO_E_ARG, "%s: %s is not aligned to its elements", who, name);
-    if (width < 1 || width > (1 << 24)) return fail(OPEVO_E_ARG, "%s: rows of %lld elements (1 to 2^24)", who, (long long)width);
-    if (ld < width || ld > ((int64_t)1 << 40)) return fail(OPEVO_E_ARG, "%s: rows of %s are %lld apart, shorter than their %lld elements or beyond 2^40", who, name, (long long)ld, (long long)width);
-    return OPEVO_OK;
-}
-int check_words(const char *who, const char *name, const void *p)
-{
-    return p && aligned(p, 4) ? OPEVO_OK : fail(OPEVO_E_ARG, "%s: %s is NULL or not aligned to 4 bytes", who, name);
-}
-
 // Up to this many slots every workgroup counts them all itself; beyond, route_count does it chunk by chunk.  Rows of 1024 bf16, two slots a token, 8 / 64 / 256 experts, us by
 // themselves against counted: 2048 slots 4.8 / 4.7 / 5.7 against 6.7 / 6.9 / 9.3, 4096 6.9 / 6.9 / 7.9 against 8.0 / 8.5 / 10.4, 8192 10.6 / 10.7 / 11.6 against 9.6 / 11.6 / 11.4,
 // 16384 20.7 / 20.7 / 21.3 against 13.2 / 15.0 / 14.4.
@@ -717,10 +688,6 @@ int run_combine_grad(const void *dy, int64_t ld_dy, const void *rows, int64_t ld
 }
 
 }  // namespace
-
-#define BY_DTYPE(dtype, call, ...)                                          \
-    ((dtype) == OPEVO_F32 ? call<float>(__VA_ARGS__)                        \
-     : (dtype) == OPEVO_BF16 ? call<__bf16>(__VA_ARGS__) : call<_Float16>(__VA_ARGS__))
 
 extern "C" int opevo_route_workspace(int64_t tokens, int k, int experts, size_t *bytes)
 {
