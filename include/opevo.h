@@ -522,6 +522,46 @@ int opevo_matmul_i8_grouped(const int8_t *a, int64_t lda, const float *scale_a, 
                             const float *scale_b, const int32_t *offsets, int experts, void *c, int64_t ldc, int out_dtype,
                             int64_t rows, int64_t N, int64_t K, void *stream);
 
+/* ------------------------------- around expert layers: norms, microscaled 4-bit numbers, layers for few tokens
+ * The conventions are those of the section before: DEVICE pointers aligned to their elements, rows `ld_*` elements apart (bytes where two codes share one), of any alignment and
+ * width (1 to 2^24), no allocation, no synchronisation, captured as they are, every output written whole, results that do not depend on the run. */
+
+/* RMS norm, with a residual added first: s = x + residual, rounded once to dtype and written to sum; i = 1 / sqrt(mean(s^2) + eps), the mean in fp32; y = s * i * weight in fp32, rounded
+ * once.  residual = NULL: s = x (sum may then be NULL); weight = NULL: 1, else `width` elements of dtype; inv_rms, if not NULL, gets i of each row, as the gradient takes it.  Sums
+ * of squares beyond fp32 give i = 0, those below it count as 0.  sum and y may each be x or residual themselves (the same first element, the same distance of rows), but not each other; rows at most 2^31 - 1. */
+int opevo_norm_rows(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual, const void *weight, float eps, int dtype, int64_t rows,
+                    int64_t width, void *sum, int64_t ld_sum, void *y, int64_t ld_y, float *inv_rms, void *stream);
+/* The same with the norm's rows in 8 bits, as opevo_matmul_i8 takes them, in one pass: v = s * weight without rounding, a = the largest |v| of the row, q = 127 v / a rounded to the
+ * nearest integer, ties to even, scale = a * i / 127.  A row without a v other than 0 has q = 0; one that holds an infinity, a NaN or a v beyond fp32 has q = 0 and scale = NaN. */
+int opevo_norm_rows_i8(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual, const void *weight, float eps, int dtype, int64_t rows,
+                       int64_t width, void *sum, int64_t ld_sum, int8_t *q, int64_t ld_q, float *scale, void *stream);
+/* Bytes of workspace (4-byte aligned; may be 0) that a gradient of this size takes if it wants dweight.  Host only. */
+int opevo_norm_rows_grad_workspace(int64_t rows, int64_t width, size_t *bytes);
+/* The gradients of opevo_norm_rows for dy, and for dsum, what comes back to the sum on its way past the norm (NULL: nothing): dx = i (weight dy - s i^2 mean(weight dy s)) + dsum in
+ * fp32, rounded once to dtype, which is the gradient of x and of the residual alike; dweight[width] = sum over the rows of dy s i, in fp32 in a fixed order (NULL: not wanted).  sum: s as
+ * the forward pass wrote it (x, where there is no residual).  dx may be dy or dsum itself (the same first element, the same distance of rows).  rows = 0 makes dweight 0. */
+int opevo_norm_rows_grad(const void *dy, int64_t ld_dy, const void *dsum, int64_t ld_dsum, const void *sum, int64_t ld_sum, const void *weight,
+                         const float *inv_rms, int dtype, int64_t rows, int64_t width, void *dx, int64_t ld_dx, float *dweight, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/* Microscaled 4-bit numbers (the OCP MX format with E2M1 elements): a row of `width` values is (width + 1) / 2 bytes, two codes each, the earlier one in the low half (the last byte's high
+ * half is written 0 and not read where the width is odd), and (width + 31) / 32 factors of a byte b each, which stands for 2^(b - 127), or NaN where b = 255.  Codes 0 .. 7: 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6; plus 8: their negatives.
+ * To them: b - 127 = floor(log2 of the largest magnitude of the 32) - 2, at least -127; codes: x / 2^(b - 127) rounded to the nearest, ties to the even code, magnitudes beyond 6 to
+ * 6; 32 values with an infinity or a NaN among them get b = 255 and codes 0.  And back: the product, rounded once to dtype. */
+int opevo_quantize_rows_mx4(const void *x, int64_t ld_x, int dtype, int64_t rows, int64_t width, uint8_t *q, int64_t ld_q, uint8_t *scale,
+                            int64_t ld_scale, void *stream);
+int opevo_dequantize_rows_mx4(const uint8_t *q, int64_t ld_q, const uint8_t *scale, int64_t ld_scale, int dtype, int64_t rows, int64_t width, void *x,
+                              int64_t ld_x, void *stream);
+/* C[m, n] = sum over k of A[m, k] * B[n, k], both in microscaled 4 bits along K, summed in fp32 and rounded once to out_dtype.  A [M][K], B [N][K] (an output channel a row), C
+ * [M][N].  M at most 2^21, N 2^24, K from 1 to 2^24; M = 0 or N = 0 does nothing.  Products of two numbers below 2^-126 in all may count as 0. */
+int opevo_matmul_mx4(const uint8_t *a, int64_t lda, const uint8_t *scale_a, int64_t ld_scale_a, const uint8_t *b, int64_t ldb, const uint8_t *scale_b,
+                     int64_t ld_scale_b, void *c, int64_t ldc, int out_dtype, int64_t M, int64_t N, int64_t K, void *stream);
+/* The same for rows of experts, as opevo_matmul_i8_grouped: B [experts][N][K], its rows all ldb (their factors all ld_scale_b) apart. */
+int opevo_matmul_mx4_grouped(const uint8_t *a, int64_t lda, const uint8_t *scale_a, int64_t ld_scale_a, const uint8_t *b, int64_t ldb, const uint8_t *scale_b,
+                             int64_t ld_scale_b, const int32_t *offsets, int experts, void *c, int64_t ldc, int out_dtype, int64_t rows, int64_t N,
+                             int64_t K, void *stream);
+
 /* -------------------------------------------------------- whole tuning run (Alg. 1) */
 typedef struct {
     const void *a, *b;         /* DEVICE inputs                                                  */

@@ -147,6 +147,14 @@ _SIGNATURES = {
     "opevo_quantize_rows_i8": [_vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int64, _vp, _vp],
     "opevo_matmul_i8": [_vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_int64, _vp],
     "opevo_matmul_i8_grouped": [_vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, C.c_int, _vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_int64, _vp],
+    "opevo_norm_rows": [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_float, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, _vp],
+    "opevo_norm_rows_i8": [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_float, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, _vp],
+    "opevo_norm_rows_grad_workspace": [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)],
+    "opevo_norm_rows_grad": [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, _vp, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int64, _vp, _vp, C.c_size_t, _vp],
+    "opevo_quantize_rows_mx4": [_vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp],
+    "opevo_dequantize_rows_mx4": [_vp, C.c_int64, _vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int64, _vp],
+    "opevo_matmul_mx4": [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_int64, _vp],
+    "opevo_matmul_mx4_grouped": [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int, _vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_int64, _vp],
     "opevo_tune": [_vp, C.c_int, C.POINTER(opevo_tune_args), _i32p, C.POINTER(opevo_tune_result)],
 }
 for _name, _argtypes in _SIGNATURES.items():
@@ -613,6 +621,47 @@ def opevo_matmul_i8_grouped(a: int, lda: int, scale_a: int, b: int, ldb: int, sc
                             rows: int, N: int, K: int, stream: int = 0) -> None:
     """rows: how many rows A and C have; which expert a row belongs to stands in offsets, on the device."""
     _check(lib.opevo_matmul_i8_grouped(a, lda, scale_a, b, ldb, scale_b, offsets, experts, c, ldc, out_dtype, rows, N, K, stream))
+
+
+# --------------------------------------------------- around expert layers: norms, microscaled 4-bit numbers
+def opevo_norm_rows(x: int, ld_x: int, residual: int, ld_residual: int, weight: int, eps: float, dtype: int, rows: int, width: int, sum: int, ld_sum: int,
+                    y: int, ld_y: int, inv_rms: int = 0, stream: int = 0) -> None:
+    _check(lib.opevo_norm_rows(x, ld_x, residual, ld_residual, weight, eps, dtype, rows, width, sum, ld_sum, y, ld_y, inv_rms, stream))
+
+
+def opevo_norm_rows_i8(x: int, ld_x: int, residual: int, ld_residual: int, weight: int, eps: float, dtype: int, rows: int, width: int, sum: int, ld_sum: int,
+                       q: int, ld_q: int, scale: int, stream: int = 0) -> None:
+    _check(lib.opevo_norm_rows_i8(x, ld_x, residual, ld_residual, weight, eps, dtype, rows, width, sum, ld_sum, q, ld_q, scale, stream))
+
+
+def opevo_norm_rows_grad_workspace(rows: int, width: int) -> int:
+    v = C.c_size_t()
+    _check(lib.opevo_norm_rows_grad_workspace(rows, width, C.byref(v)))
+    return v.value
+
+
+def opevo_norm_rows_grad(dy: int, ld_dy: int, dsum: int, ld_dsum: int, sum: int, ld_sum: int, weight: int, inv_rms: int, dtype: int, rows: int, width: int,
+                         dx: int, ld_dx: int, dweight: int = 0, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> None:
+    _check(lib.opevo_norm_rows_grad(dy, ld_dy, dsum, ld_dsum, sum, ld_sum, weight, inv_rms, dtype, rows, width, dx, ld_dx, dweight, workspace, workspace_bytes, stream))
+
+
+def opevo_quantize_rows_mx4(x: int, ld_x: int, dtype: int, rows: int, width: int, q: int, ld_q: int, scale: int, ld_scale: int, stream: int = 0) -> None:
+    _check(lib.opevo_quantize_rows_mx4(x, ld_x, dtype, rows, width, q, ld_q, scale, ld_scale, stream))
+
+
+def opevo_dequantize_rows_mx4(q: int, ld_q: int, scale: int, ld_scale: int, dtype: int, rows: int, width: int, x: int, ld_x: int, stream: int = 0) -> None:
+    _check(lib.opevo_dequantize_rows_mx4(q, ld_q, scale, ld_scale, dtype, rows, width, x, ld_x, stream))
+
+
+def opevo_matmul_mx4(a: int, lda: int, scale_a: int, ld_scale_a: int, b: int, ldb: int, scale_b: int, ld_scale_b: int, c: int, ldc: int, out_dtype: int,
+                     M: int, N: int, K: int, stream: int = 0) -> None:
+    _check(lib.opevo_matmul_mx4(a, lda, scale_a, ld_scale_a, b, ldb, scale_b, ld_scale_b, c, ldc, out_dtype, M, N, K, stream))
+
+
+def opevo_matmul_mx4_grouped(a: int, lda: int, scale_a: int, ld_scale_a: int, b: int, ldb: int, scale_b: int, ld_scale_b: int, offsets: int, experts: int,
+                             c: int, ldc: int, out_dtype: int, rows: int, N: int, K: int, stream: int = 0) -> None:
+    """rows: how many rows A and C have; which expert a row belongs to stands in offsets, on the device."""
+    _check(lib.opevo_matmul_mx4_grouped(a, lda, scale_a, ld_scale_a, b, ldb, scale_b, ld_scale_b, offsets, experts, c, ldc, out_dtype, rows, N, K, stream))
 
 
 def opevo_tune(op, variant: int, a: int, b: int, c: int, ref: Optional[int] = None, stream: int = 0,

@@ -1,0 +1,632 @@
+// Products of microscaled 4-bit numbers (mx4.hpp) along K:
+//   C[m, n] = sum_k A[m, k] B[n, k],
+// each operand the value of its code times the factor of its 32.  The matrix instruction takes the codes and the factors as they are stored (128 values and four factors a row at a time) and
+// sums in fp32; the sum is rounded once to the output type.  B holds an output channel a row.  The grouped form gives each range of rows offsets[e] .. offsets[e + 1] a B of its own.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "launch.hpp"
+#include "narrow.hpp"
+#include "product.hpp"
+#include "rows.hpp"
+#include "wave.hpp"
+
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// What one call computes.  Plain: experts = 0, offsets = NULL.  Grouped: B has experts * N rows.
+struct Product4 {
+    const uint8_t *a, *b, *sa, *sb;
+    long lda, ldb, ldsa, ldsb;
+    const int *offsets;
+    int experts;
+    void *c;
+    long ldc;
+    int out;            // opevo_dtype
+    long m;
+    int n, k;           // k: bytes of a row, the last one half used where `odd`
+    int blocks;         // factors of a row
+    bool odd;
+};
+
+// Sixteen rows of either operand, 128 values: lane l holds 32 values of row l % 16 and their factor, in byte SA (SB) of its scale word.
+template <int SB, int SA>
+__device__ __forceinline__ f32x4 mfma(i32x4 b, i32x4 a, f32x4 c, int sb, int sa)
+{
+    const i32x8 b8 = {b[0], b[1], b[2], b[3], 0, 0, 0, 0}, a8 = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b8, a8, c, 4, 4, SB, sb, SA, sa);
+}
+// The bytes are known once the loops around are unrolled.
+__device__ __forceinline__ f32x4 mfma_at(int at_b, int at_a, i32x4 b, i32x4 a, f32x4 c, int sb, int sa)
+{
+    switch (at_b * 4 + at_a) {
+    case 0: return mfma<0, 0>(b, a, c, sb, sa);
+    case 1: return mfma<0, 1>(b, a, c, sb, sa);
+    case 2: return mfma<0, 2>(b, a, c, sb, sa);
+    case 3: return mfma<0, 3>(b, a, c, sb, sa);
+    case 4: return mfma<1, 0>(b, a, c, sb, sa);
+    case 5: return mfma<1, 1>(b, a, c, sb, sa);
+    case 6: return mfma<1, 2>(b, a, c, sb, sa);
+    case 7: return mfma<1, 3>(b, a, c, sb, sa);
+    case 8: return mfma<2, 0>(b, a, c, sb, sa);
+    case 9: return mfma<2, 1>(b, a, c, sb, sa);
+    case 10: return mfma<2, 2>(b, a, c, sb, sa);
+    case 11: return mfma<2, 3>(b, a, c, sb, sa);
+    case 12: return mfma<3, 0>(b, a, c, sb, sa);
+    case 13: return mfma<3, 1>(b, a, c, sb, sa);
+    case 14: return mfma<3, 2>(b, a, c, sb, sa);
+    default: return mfma<3, 3>(b, a, c, sb, sa);
+    }
+}
+
+// 16 bytes of a row from byte k on, zeros past its end (and in the half byte past an odd K).
+__device__ __forceinline__ i32x4 load_codes(const uint8_t *row, int k, int end, bool odd)
+{
+    i32x4 v = load_chunk((const int8_t *)row, k, end);
+    const int last = end - 1 - k;
+    if (odd && last >= 0 && last < 16)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (last >> 2 == i) v[i] &= ~(0xf0 << 8 * (last & 3));
+    return v;
+}
+// Four factors of a row from block b on, zeros past its end: with codes of zero any factor but NaN gives zero.
+__device__ __forceinline__ int load_factors(const uint8_t *row, int b, int blocks)
+{
+    int v = 0;
+    if (b + 4 <= blocks) __builtin_memcpy(&v, row + b, 4);
+    else
+        for (int i = 0; b + i < blocks; ++i) v |= (int)row[b + i] << 8 * i;
+    return v;
+}
+
+// Writes a wave's MI x NI atoms, rows r.first + m0 .. and columns col0 .. of C.  Lane l of an atom holds columns 4 * (l / 16) .. + 3 of row l % 16; the 16 rows of an atom row go through a
+// piece of LDS of the wave's own and leave as whole lines, 16 bytes a lane.
+template <typename T, int NI> constexpr int kPatch = 16 * NI * 16 * (int)sizeof(T);   // bytes of LDS a wave takes
+template <typename T, int MI, int NI>
+__device__ __forceinline__ void store_sums(const Product4 &p, const Rows &r, int m0, int col0, const f32x4 (&acc)[MI][NI], int8_t *patch, int lane)
+{
+    constexpr int PITCH = NI * 16 * (int)sizeof(T), CPR = NI * (int)sizeof(T), V = 16 / (int)sizeof(T);   // bytes, 16-byte chunks of a row, elements of a chunk
+    static_assert((CPR & (CPR - 1)) == 0, "chunks are permuted by an exclusive or");
+    const int cols = p.n - col0;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            T v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = narrow<T>(acc[i][j][e]);
+            constexpr int OF = 16 / (4 * (int)sizeof(T));       // such pieces of a chunk
+            const int piece = j * 4 + (lane >> 4), chunk = (piece / OF) ^ (lane & 15) % CPR;     // a row's chunks are permuted, so that 16 rows fall on different banks
+            __builtin_memcpy(__builtin_assume_aligned(patch + (lane & 15) * PITCH + chunk * 16 + piece % OF * (16 / OF), 4 * sizeof(T)), v, sizeof v);
+        }
+        exchange();
+        const long row0 = r.first + m0 + i * 16;
+#pragma unroll
+        for (int u = 0; u < (16 * CPR + 63) / 64; ++u) {
+            const int at = u * 64 + lane, row = at / CPR, c = at % CPR * V;
+            if ((16 * CPR) % 64 != 0 && row >= 16) continue;
+            if (row0 + row >= r.last || c >= cols) continue;
+            T *dst = (T *)p.c + (row0 + row) * p.ldc + col0 + c;
+            const int8_t *from = patch + row * PITCH + (at % CPR ^ row % CPR) * 16;
+            if (c + V <= cols) __builtin_memcpy(dst, __builtin_assume_aligned(from, 16), 16);
+            else
+#pragma unroll 1
+                for (int e = 0; e < cols - c; ++e) dst[e] = ((const T *)from)[e];
+        }
+        exchange();
+    }
+}
+
+// ------------------------------------------------------------------ few rows
+// For few rows the weights are all there is to read, each once, and the time is that of one trip to memory.  Every wave loads its fragments and their factors from global memory into
+// registers, 512 values along K a step (four MFMAs), the next step's while it multiplies.  The W waves of a workgroup share a tile of 16 x 16 and deal the steps among themselves;
+// their sums meet in LDS.  Loads take any alignment.
+template <int W>
+__global__ __launch_bounds__(W * 64)
+void product4_thin(Product4 p)
+{
+    __shared__ f32x4 sums[W][64];
+    Rows r;
+    if (!find_rows(p, 16, row_tile(), &r)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n0 = blockIdx.x * 16, g = lane >> 4;
+    f32x4 acc = {};
+    if (!r.zero) {
+        const long m = r.first + (lane & 15), ma = m < r.last ? m : r.last - 1, nb = (long)r.expert * p.n + min(n0 + (lane & 15), p.n - 1);
+        const uint8_t *row[2] = {p.a + ma * p.lda, p.b + nb * p.ldb}, *by[2] = {p.sa + ma * p.ldsa, p.sb + nb * p.ldsb};
+        const int steps = (p.k + 255) / 256;
+        i32x4 v[2][4], w[2][4], fv[2], fw[2];
+        auto load = [&](i32x4 (&to)[2][4], i32x4 (&f)[2], int step) {
+            const int k0 = step * 256 + g * 16;
+            if (step * 256 + 256 <= p.k && !p.odd) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    __builtin_memcpy(&f[i], by[i] + step * 16, 16);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) __builtin_memcpy(&to[i][u], row[i] + k0 + u * 64, 16);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        f[i][u] = load_factors(by[i], step * 16 + u * 4, p.blocks);
+                        to[i][u] = load_codes(row[i], k0 + u * 64, p.k, p.odd);
+                    }
+            }
+        };
+        auto multiply = [&](const i32x4 (&of)[2][4], const i32x4 (&f)[2]) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) acc = mfma<0, 0>(of[1][u], of[0][u], acc, (int)((unsigned)f[1][u] >> 8 * g), (int)((unsigned)f[0][u] >> 8 * g));
+        };
+        int s = wave;
+        if (s < steps) load(v, fv, s);
+        for (; s < steps; s += 2 * W) {
+            if (s + W < steps) load(w, fw, s + W);
+            multiply(v, fv);
+            if (s + W >= steps) break;
+            if (s + 2 * W < steps) load(v, fv, s + 2 * W);
+            multiply(w, fw);
+        }
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (wave > 0) return;
+    f32x4 sum = sums[0][lane];
+#pragma unroll
+    for (int o = 1; o < W; ++o) sum += sums[o][lane];
+    const long m = r.first + (lane & 15);
+    if (m >= r.last) return;
+    const float c[4] = {sum[0], sum[1], sum[2], sum[3]};
+    const int col = n0 + g * 4;
+    if (p.out == OPEVO_F32) store4((float *)p.c + m * p.ldc, col, p.n, c);
+    else if (p.out == OPEVO_BF16) store4((__bf16 *)p.c + m * p.ldc, col, p.n, c);
+    else store4((_Float16 *)p.c + m * p.ldc, col, p.n, c);
+}
+
+// ------------------------------------------------------------------ tiles
+// Workgroup tile BM x BN, slabs of 128 bytes (256 values), WM x WN waves of MI x NI atoms of 16 x 16 x 128, KG groups of such waves that take every KG-th slab and add up
+// their sums in LDS at the end.  The 16-byte chunk c of a row sits at chunk position c ^ (row / 2 % 8) of its row of the slab: the 16 lanes of a turn of a fragment read then
+// fall on 16 different groups of banks.  Behind the rows of a slab stand their factors, eight bytes a row.  Rows past the end repeat the last one (their results are not stored); chunks past K are zeros.
+// DIRECT: every wave issues wave-wide loads whose destination is LDS (16 bytes a lane for the codes, the chunk each lane loads chosen by the permutation, 4 for the factors); a
+// ring of STAGES slabs keeps STAGES - 1 in flight.  For operands whose pointers and row lengths are multiples of 16 (factors: of 4) and K of 32.
+// Otherwise the slabs pass through registers, from where they start on any address: two stages in LDS, the slab after them on its way.
+template <bool DIRECT_, int BM_, int BN_, int WM_, int WN_, int STAGES_, int KG_ = 1>
+struct Shape {
+    static constexpr bool DIRECT = DIRECT_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, BK = 128;
+    static constexpr int KG = KG_, NW = WM * WN, NT = NW * 64 * KG, MI = BM / WM / 16, NI = BN / WN / 16;
+    static constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, PER = LA + LB, CODES = (BM + BN) * BK, STAGE = CODES + (BM + BN) * 8;
+    static constexpr int FP = (BM + BN) / 32, FPER = (FP + NW - 1) / NW;      // pieces of 32 rows' factors, of a wave; pieces beyond the last one are loaded twice
+    static constexpr int BYTES = KG * STAGES * STAGE;
+    static_assert(MI * WM * 16 == BM && NI * WN * 16 == BN && LA * 8 * NW == BM && LB * 8 * NW == BN && BM % 32 == 0 && BN % 32 == 0 && STAGES >= 2 && (DIRECT || STAGES == 2)
+                      && BYTES <= 160 * 1024 && NW * KG <= 16 && BM + BN <= NW * 64 && STAGE % 16 == 0,
+                  "");
+};
+
+// lane i's 4 bytes from base + off to LDS at lds + 4 i, as load_to_lds.
+__device__ __forceinline__ void load_word_to_lds(const int8_t *base, unsigned off, unsigned lds)
+{
+    const int8_t *copy;
+    asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dword %1, %0" : "=&s"(copy) : "v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
+
+// Factors of N atoms for both steps of a slab, as the matrix instruction takes them.  Four atoms at a time: lane (r, g) reads the eight factors of row r of atom g, and the four lanes
+// of an r exchange bytes until each has its own group's factor of all four atoms in a word (byte i: atom i).  Fewer: every lane reads its row's word and shifts.
+template <int N> struct Factors {
+    static constexpr bool FOURS = N % 4 == 0;
+    static constexpr int W = FOURS ? N / 4 : N;
+    int raw[W][2], word[2][W];
+    // `at`: the factors of the wave's first row
+    __device__ __forceinline__ void read(const int8_t *at, int lane)
+    {
+#pragma unroll
+        for (int i = 0; i < W; ++i) __builtin_memcpy(raw[i], __builtin_assume_aligned(at + (FOURS ? (i * 4 + (lane >> 4)) * 16 + (lane & 15) : i * 16 + (lane & 15)) * 8, 8), 8);
+    }
+    __device__ __forceinline__ void turn(int kk, int lane)
+    {
+        const int g = lane >> 4;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if constexpr (FOURS) {
+                typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+                const u32x2 far = __builtin_amdgcn_permlane32_swap((unsigned)raw[i][kk], (unsigned)raw[i][kk], false, false);      // the words of lanes g & 1 and g | 2
+                const unsigned x = __builtin_amdgcn_perm(far.y, far.x, g & 2 ? 0x07060302u : 0x05040100u);        // of either the bytes of groups 0 and 1, or 2 and 3
+                const u32x2 near = __builtin_amdgcn_permlane16_swap(x, x, false, false);                           // those of an even and an odd g
+                word[kk][i] = (int)__builtin_amdgcn_perm(near.y, near.x, g & 1 ? 0x07030501u : 0x06020400u);
+            } else {
+                word[kk][i] = (int)((unsigned)raw[i][kk] >> 8 * g);
+            }
+        }
+    }
+    __device__ __forceinline__ int of(int kk, int i) const { return word[kk][FOURS ? i / 4 : i]; }
+    static constexpr int at(int i) { return FOURS ? i % 4 : 0; }
+};
+
+template <typename S>
+__global__ __launch_bounds__(S::NT)
+void product4_tile(Product4 p)
+{
+    constexpr int BM = S::BM, BN = S::BN, BK = S::BK, MI = S::MI, NI = S::NI, LA = S::LA, LB = S::LB, PER = S::PER, ALL = PER + S::FPER;
+    __shared__ __attribute__((aligned(1024))) int8_t whole[S::BYTES];
+    static_assert(S::NW * kPatch<float, NI> <= S::BYTES && (S::KG - 1) * S::NW * MI * NI * 1024 <= S::BYTES, "");
+    Rows r;
+    if (!find_rows(p, BM, row_tile(), &r)) return;
+    const int tid = threadIdx.x, lane = tid & 63, all = uniform(tid >> 6), group = all / S::NW, wave = all % S::NW, wm = wave / S::WN, wn = wave % S::WN;
+    const int n0 = blockIdx.x * BN;
+    int8_t *const ring = whole + group * (S::STAGES * S::STAGE);
+    f32x4 acc[MI][NI] = {};
+    if (!r.zero) {
+        const unsigned ring_at = uniform((int)(unsigned)(unsigned long)(__attribute__((address_space(3))) int8_t *)ring);
+        // this wave's pieces of a slab: eight rows each, lane -> row lane / 8, chunk position lane % 8
+        const int rows = (int)(r.last - r.first), cols = p.n - n0;
+        unsigned off[PER];
+#pragma unroll
+        for (int t = 0; t < PER; ++t) {
+            const bool is_a = t < LA;
+            const int row = (is_a ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, limit = is_a ? rows : cols;
+            const int chunk = (lane & 7) ^ (row >> 1 & 7);
+            off[t] = (unsigned)(row < limit ? row : limit - 1) * (unsigned)(is_a ? p.lda : p.ldb) + chunk * 16;
+        }
+        const long b0 = (long)r.expert * p.n + n0;
+        const int8_t *abase = uniform((const int8_t *)p.a + r.first * p.lda), *bbase = uniform((const int8_t *)p.b + b0 * p.ldb);
+        const int8_t *afact = uniform((const int8_t *)p.sa + r.first * p.ldsa), *bfact = uniform((const int8_t *)p.sb + b0 * p.ldsb);
+        // a row of the tile, A's before B's -> where its factors start
+        auto factors_at = [&](int row) { return row < BM ? (unsigned)min(row, rows - 1) * (unsigned)p.ldsa : (unsigned)min(row - BM, cols - 1) * (unsigned)p.ldsb; };
+        // and the wave's pieces of the factors: 32 rows each, lane -> row lane / 2, four of the eight factors
+        unsigned foff[S::FPER];
+        int fpiece[S::FPER];
+#pragma unroll
+        for (int t = 0; t < S::FPER; ++t) {
+            fpiece[t] = (wave * S::FPER + t) % S::FP;
+            foff[t] = factors_at(fpiece[t] * 32 + lane / 2) + (lane & 1) * 4;
+        }
+        const int whole_slabs = p.odd ? (p.k - 1) / BK : p.k / BK, slabs = (p.k + BK - 1) / BK;
+        const int steps = (slabs + S::KG - 1) / S::KG;      // of every group; a slab past the last one is zeros
+        // This wave's share of a slab into a stage: of a whole slab; of one that K ends in, or that lies past it, which is filled up with zeros.
+        auto issue = [&](int step, int stage) {
+            const int slab = step * S::KG + group;
+            const int8_t *as = abase + (long)slab * BK, *bs = bbase + (long)slab * BK;
+            const unsigned at = ring_at + stage * S::STAGE, at_a = at + wave * LA * 1024, at_b = at + BM * BK + wave * LB * 1024;
+#pragma unroll
+            for (int t = 0; t < PER; ++t) load_to_lds(t < LA ? as : bs, off[t], t < LA ? at_a + t * 1024 : at_b + (t - LA) * 1024);
+#pragma unroll
+            for (int t = 0; t < S::FPER; ++t) load_word_to_lds(uniform((fpiece[t] < BM / 32 ? afact : bfact) + (long)slab * 8), foff[t], at + S::CODES + fpiece[t] * 256);
+        };
+        auto issue_ragged = [&](int step, int stage) {
+            const int slab = step * S::KG + group;
+            const int8_t *as = abase + (long)slab * BK, *bs = bbase + (long)slab * BK;
+            const unsigned at = ring_at + stage * S::STAGE, at_a = at + wave * LA * 1024, at_b = at + BM * BK + wave * LB * 1024;
+#pragma unroll
+            for (int t = 0; t < PER; ++t) {
+                const int row = (t < LA ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, chunk = (lane & 7) ^ (row >> 1 & 7);
+                const unsigned to = t < LA ? at_a + t * 1024 : at_b + (t - LA) * 1024;
+                if (slab * BK + chunk * 16 < p.k) load_to_lds(t < LA ? as : bs, off[t], to);
+                else *(i32x4 *)(ring + (to - ring_at) + lane * 16) = i32x4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int t = 0; t < S::FPER; ++t)
+                *(int *)(ring + stage * S::STAGE + S::CODES + fpiece[t] * 256 + lane * 4) =
+                    load_factors((const uint8_t *)(fpiece[t] < BM / 32 ? afact : bfact) + (foff[t] - (lane & 1) * 4), slab * 8 + (lane & 1) * 4, p.blocks);
+        };
+        // The same by way of registers: fetch starts the loads, put stores what they brought.  A thread takes the factors of one row.
+        i32x4 hold[PER];
+        int fhold[2];
+        const int mine = (wave * 64 + lane) % (BM + BN);      // threads beyond the last row take one again
+        auto fetch = [&](int step) {
+            const int slab = step * S::KG + group;
+#pragma unroll
+            for (int t = 0; t < PER; ++t) __builtin_memcpy(&hold[t], (t < LA ? abase : bbase) + (long)slab * BK + off[t], 16);
+            __builtin_memcpy(fhold, (mine < BM ? afact : bfact) + factors_at(mine) + (long)slab * 8, 8);
+        };
+        auto fetch_ragged = [&](int step) {
+            const int slab = step * S::KG + group;
+#pragma unroll
+            for (int t = 0; t < PER; ++t) {
+                const int row = (t < LA ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, chunk = (lane & 7) ^ (row >> 1 & 7);
+                hold[t] = load_codes((const uint8_t *)(t < LA ? abase : bbase) + off[t] - chunk * 16, slab * BK + chunk * 16, p.k, p.odd);
+            }
+            const uint8_t *of = (const uint8_t *)(mine < BM ? afact : bfact) + factors_at(mine);
+            fhold[0] = load_factors(of, slab * 8, p.blocks);
+            fhold[1] = load_factors(of, slab * 8 + 4, p.blocks);
+        };
+        auto put = [&](int stage) {
+#pragma unroll
+            for (int t = 0; t < PER; ++t) *(i32x4 *)(ring + stage * S::STAGE + (t < LA ? (wave * LA + t) * 1024 : BM * BK + (wave * LB + t - LA) * 1024) + lane * 16) = hold[t];
+            __builtin_memcpy(__builtin_assume_aligned(ring + stage * S::STAGE + S::CODES + mine * 8, 8), fhold, 8);
+        };
+        // A stage that every wave has read is filled with the slab `step`, if there is one.  HOW says what has to be loaded for that: a whole slab, anything or nothing.  The loop over slabs is
+        // three, one for each, because a branch among a slab's MFMAs has the compiler move them behind it (256 x 256: all reads, then all MFMAs, and spills).
+        enum How { kWhole, kAny, kNone };
+        auto is_whole = [&](int step) { return step * S::KG + group < whole_slabs; };
+        auto refill = [&](auto how, int step, int stage) {
+            constexpr How HOW = decltype(how)::value;
+            if constexpr (S::DIRECT) {
+                if constexpr (HOW == kWhole) issue(step, stage);
+                else if constexpr (HOW == kAny) {
+                    if (step < steps) {
+                        if (is_whole(step)) issue(step, stage);
+                        else issue_ragged(step, stage);
+                    }
+                }
+            } else {
+                if constexpr (HOW != kNone) put(stage);
+                if constexpr (HOW == kWhole) fetch(step + 1);
+                else if constexpr (HOW == kAny) {
+                    if (step + 1 < steps) {
+                        if (is_whole(step + 1)) fetch(step + 1);
+                        else fetch_ragged(step + 1);
+                    }
+                }
+            }
+        };
+        using Whole = std::integral_constant<How, kWhole>;
+        using Any = std::integral_constant<How, kAny>;
+        using None = std::integral_constant<How, kNone>;
+        // the slab whose load slab q sets off
+        constexpr int AHEAD = S::DIRECT ? S::STAGES : S::STAGES + 1;
+        // this wave has read its part of a slab, and its part of the next one has landed
+        auto wait_next = [&](bool more) {
+            if (!S::DIRECT) WAIT_LGKM();
+            else if (S::STAGES > 2 && more) WAIT_LGKM_VMCNT((S::STAGES - 2) * ALL);
+            else WAIT_LGKM_VMCNT(0);
+        };
+        // fragments: lane l holds row l % 16, the 32 values from 32 * (l / 16) of a step of 128
+        const int sw = lane >> 1 & 7, fr = lane & 15;
+        Factors<MI> fa;
+        Factors<NI> fb;
+        auto read_factors = [&](int stage) {
+            const int8_t *at = ring + stage * S::STAGE + S::CODES;
+            fa.read(at + wm * MI * 128, lane);
+            fb.read(at + (BM + wn * NI * 16) * 8, lane);
+        };
+        // prologue: slabs 0 .. STAGES - 1 under way, slab 0 landed, its first fragments read
+        if (!S::DIRECT) {
+            if (is_whole(0)) fetch(0);
+            else fetch_ragged(0);
+        }
+#pragma unroll
+        for (int s = 0; s < S::STAGES; ++s)
+            if (s < steps) refill(Any(), s, s);
+        if (!S::DIRECT) WAIT_LGKM();
+        else if (S::STAGES > 2 && steps > S::STAGES) WAIT_LGKM_VMCNT((S::STAGES - 1) * ALL);
+        else WAIT_LGKM_VMCNT(0);
+        BARRIER();
+        read_factors(0);
+        if constexpr (MI * NI <= 4) {
+            // Few MFMAs a slab: the fragments of a whole slab are read at once, while the slab before it is multiplied.
+            i32x4 ag[2][2][MI], bg[2][2][NI];
+            auto read_slab = [&](int set, int stage) {
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    const int8_t *at = ring + stage * S::STAGE + (((kk * 4 + (lane >> 4)) ^ sw) << 4);
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) bg[set][kk][i] = *(const i32x4 *)(at + BM * BK + (wn * NI * 16 + i * 16 + fr) * BK);
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) ag[set][kk][i] = *(const i32x4 *)(at + (wm * MI * 16 + i * 16 + fr) * BK);
+                }
+            };
+            read_slab(0, 0);
+            int stage = 0;
+            auto slab = [&](auto how, int q, int set) {
+                const int next = stage + 1 == S::STAGES ? 0 : stage + 1;
+                const bool more = q + S::STAGES < steps;
+                wait_next(more);
+                BARRIER();                  // every wave has read slab q, and slab q + 1 has landed
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) { fa.turn(kk, lane); fb.turn(kk, lane); }
+                read_factors(next);
+                read_slab(set ^ 1, next);
+                refill(how, q + S::STAGES, stage);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                    for (int m = 0; m < MI * NI; ++m) {
+                        const int i = m / NI, j = m % NI;
+                        acc[i][j] = mfma_at(fb.at(j), fa.at(i), bg[set][kk][j], ag[set][kk][i], acc[i][j], fb.of(kk, j), fa.of(kk, i));
+                    }
+                stage = next;
+            };
+            int q = 0;
+            for (; is_whole(q + 1 + AHEAD); q += 2) { slab(Whole(), q, 0); slab(Whole(), q + 1, 1); }
+            for (; q + S::STAGES < steps; q += 2) {
+                slab(Any(), q, 0);
+                if (q + 1 < steps) slab(Any(), q + 1, 1);
+            }
+            for (; q < steps; q += 2) {
+                slab(None(), q, 0);
+                if (q + 1 < steps) slab(None(), q + 1, 1);
+            }
+        } else {
+        // A slab is 2 MI fragments of A, those of its first 128 values before the others, each multiplied by the NI of B.  The one that comes D fragments later is read meanwhile, into
+        // one of R places: holding both steps' fragments of a 256 x 256 tile would take more registers than there are.
+        constexpr int D = MI == 8 ? 3 : MI, R = MI == 8 ? 4 : 2 * MI, LAST = 2 * MI - D;
+        static_assert(2 * MI % R == 0 && D < R && LAST >= MI && MI >= NI && D * NI > NI, "");
+        i32x4 af[R], bf[2][NI];
+        auto chunk_at = [&](int stage, int kk) { return ring + stage * S::STAGE + (((kk * 4 + (lane >> 4)) ^ sw) << 4); };
+        auto read_a = [&](int stage, int f) { af[f % R] = *(const i32x4 *)(chunk_at(stage, f / MI) + (wm * MI * 16 + f % MI * 16 + fr) * BK); };
+        auto read_b = [&](int stage, int kk, int i) { bf[kk][i] = *(const i32x4 *)(chunk_at(stage, kk) + BM * BK + (wn * NI * 16 + i * 16 + fr) * BK); };
+#pragma unroll
+        for (int i = 0; i < NI; ++i) read_b(0, 0, i);
+#pragma unroll
+        for (int f = 0; f < D; ++f) read_a(0, f);
+        fa.turn(0, lane);
+        fb.turn(0, lane);
+        // Behind the first MFMA of fragment LAST every wave has read the slab and the next one has landed: its factors and first fragments are read and the stage is refilled.  (After
+        // the last slab the reads fetch what the ring holds; nothing uses it.)
+        int stage = 0;
+        auto slab = [&](auto how, int q) {
+            const int next = stage + 1 == S::STAGES ? 0 : stage + 1;
+            const bool more = q + S::STAGES < steps;
+#pragma unroll
+            for (int f = 0; f < 2 * MI; ++f) {
+                const int kk = f / MI, x = f % MI;
+#pragma unroll
+                for (int y = 0; y < NI; ++y) {
+                    acc[x][y] = mfma_at(fb.at(y), fa.at(x), bf[kk][y], af[f % R], acc[x][y], fb.of(kk, y), fa.of(kk, x));
+                    if (f == LAST && y == 0) {
+                        wait_next(more);
+                        BARRIER();
+                        read_factors(next);
+                        if constexpr (decltype(how)::value == kWhole) refill(how, q + S::STAGES, stage);
+                    }
+                    if (y == 0) read_a(f + D < 2 * MI ? stage : next, (f + D) % (2 * MI));
+                    if (y == 1 && f < NI) read_b(stage, 1, f);
+                    const int past = (f - LAST) * NI + y - 1;
+                    if (past >= 0 && past < NI) read_b(next, 0, past);
+                    if (f == 0 && y == NI - 1) { fa.turn(1, lane); fb.turn(1, lane); }
+                    if (f == 2 * MI - 1 && y == NI - 1) { fa.turn(0, lane); fb.turn(0, lane); }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if constexpr (decltype(how)::value == kAny) {
+#pragma unroll
+                for (int m = 0; m < MI * NI; ++m) asm volatile("" : "+v"(acc[m / NI][m % NI]));      // the sums are due here
+                refill(how, q + S::STAGES, stage);
+            }
+            stage = next;
+        };
+        int q = 0;
+        for (; is_whole(q + AHEAD); ++q) slab(Whole(), q);
+        for (; q + S::STAGES < steps; ++q) slab(Any(), q);
+        for (; q < steps; ++q) slab(None(), q);
+        }
+        WAIT_LGKM_VMCNT(0);
+    }
+    __syncthreads();
+    if (S::KG > 1) {                        // the groups' sums meet in LDS
+        f32x4 *const sums = (f32x4 *)whole;
+        if (group > 0)
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) sums[((((group - 1) * S::NW + wave) * MI + i) * NI + j) * 64 + lane] = acc[i][j];
+        __syncthreads();
+        if (group == 0)
+#pragma unroll
+            for (int g = 0; g < S::KG - 1; ++g)
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) acc[i][j] += sums[(((g * S::NW + wave) * MI + i) * NI + j) * 64 + lane];
+        __syncthreads();
+        if (group > 0) return;
+    }
+    int8_t *const patch = whole + wave * kPatch<float, NI>;
+    if (p.out == OPEVO_F32) store_sums<float>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch, lane);
+    else if (p.out == OPEVO_BF16) store_sums<__bf16>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch, lane);
+    else store_sums<_Float16>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch, lane);
+}
+
+using opevo::launch;
+
+// How many tiles of bm rows there can be at most.  Grouped: each expert's last one is ragged, and so is that of the rows of none.
+int64_t row_tiles(const Product4 &p, int bm) { return p.offsets ? std::min<int64_t>(p.m, p.m / bm + p.experts + 1) : (p.m + bm - 1) / bm; }
+
+dim3 grid_of(const Product4 &p, int bm, int bn)
+{
+    const int64_t tiles = row_tiles(p, bm);
+    return dim3((unsigned)((p.n + bn - 1) / bn), (unsigned)std::min<int64_t>(tiles, kGridY), (unsigned)((tiles + kGridY - 1) / kGridY));
+}
+
+template <typename S>
+int run_tile(const Product4 &p, hipStream_t stream)
+{
+    return launch("product4 launch", product4_tile<S>, grid_of(p, S::BM, S::BN), dim3(S::NT), stream, p);
+}
+
+template <int W>
+int run_thin(const Product4 &p, hipStream_t stream)
+{
+    return launch("product4 launch", product4_thin<W>, grid_of(p, 16, 16), dim3(W * 64), stream, p);
+}
+
+// A kernel and what it takes, in us: launch + max(steps * chain, load * (tile + steps * rate)), where steps is how many slabs (thin: steps of 256 bytes) a wave
+// goes through and load the workgroups for each of the 256 compute units, rounded up where that foretold the times better.  The first term is a workgroup's chain of latencies,
+// the second what a compute unit gets through.
+struct Kernel {
+    int (*run)(const Product4 &, hipStream_t);
+    int bm, bn, step, ways;             // tile, bytes of a step, waves or groups that share the steps
+    int64_t most;                       // rows it is considered for
+    bool round_up;
+    float launch, chain, tile, rate;
+};
+constexpr int64_t kAll = INT64_MAX;
+const Kernel kDirect[] = {
+    {run_tile<Shape<true, 256, 256, 2, 4, 2>>, 256, 256, 128, 1, kAll, true, 0.f, 1.6f, 10.8f, 1.41f},
+    {run_tile<Shape<true, 128, 128, 2, 4, 4>>, 128, 128, 128, 1, kAll, true, 0.f, 0.f, 5.18f, 0.576f},
+    {run_tile<Shape<true, 64, 64, 2, 4, 4>>, 64, 64, 128, 1, kAll, false, 2.6f, 0.322f, 0.783f, 0.322f},
+    {run_tile<Shape<true, 32, 32, 2, 2, 6, 2>>, 32, 32, 128, 2, kAll, false, 2.39f, 0.26f, 0.532f, 0.372f},
+    {run_thin<4>, 16, 16, 256, 4, 256, false, 2.22f, 0.683f, 0.f, 0.775f},
+};
+const Kernel kAny[] = {
+    {run_tile<Shape<false, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, kAll, true, 0.f, 0.f, 4.32f, 0.78f},
+    {run_tile<Shape<false, 64, 64, 2, 4, 2>>, 64, 64, 128, 1, kAll, true, 2.07f, 0.466f, 1.25f, 0.461f},
+    {run_tile<Shape<false, 32, 32, 2, 2, 2, 2>>, 32, 32, 128, 2, kAll, true, 2.4f, 0.545f, 0.501f, 0.363f},
+    {run_thin<4>, 16, 16, 256, 4, 64, true, 0.993f, 2.07f, 0.f, 1.74f},
+};
+
+int run_product4(const Product4 &p, hipStream_t stream)
+{
+    const auto whole = [](const void *at, long ld, int to) { return reinterpret_cast<uintptr_t>(at) % to == 0 && ld % to == 0; };
+    const bool direct = p.k % 16 == 0 && !p.odd && whole(p.a, p.lda, 16) && whole(p.b, p.ldb, 16) && whole(p.sa, p.ldsa, 4) && whole(p.sb, p.ldsb, 4);
+    // a tile's rows are addressed by 32-bit offsets from its first
+    constexpr long kNear = 1 << 24;
+    if (p.lda > kNear || p.ldb > kNear || p.ldsa > kNear || p.ldsb > kNear) return run_thin<4>(p, stream);
+    // grouped: as if the rows were dealt evenly, which the host cannot know
+    const int64_t parts = p.offsets ? std::min<int64_t>(p.experts, p.m) : 1, rows = (p.m + parts - 1) / parts;
+    const Kernel *best = nullptr;
+    float least = 0.f;
+    const auto consider = [&](const Kernel &k) {
+        if (rows > k.most) return;
+        const int64_t groups = parts * ((rows + k.bm - 1) / k.bm) * ((p.n + k.bn - 1) / k.bn), slabs = (p.k + k.step - 1) / k.step;
+        const float steps = (float)((slabs + k.ways - 1) / k.ways), load = k.round_up ? (float)((groups + 255) / 256) : (float)groups / 256.f;
+        const float us = k.launch + std::max(steps * k.chain, load * (k.tile + steps * k.rate));
+        if (!best || us < least) { best = &k; least = us; }
+    };
+    if (direct) for (const Kernel &k : kDirect) consider(k);
+    else for (const Kernel &k : kAny) consider(k);
+    return best->run(p, stream);
+}
+
+int product4(const char *who, Product4 &p, int64_t m, int64_t n, int64_t k, int experts, void *stream)
+{
+    if (!known(p.out)) return fail(OPEVO_E_ARG, "%s: unknown output type %d", who, p.out);
+    if (m < 0 || n < 0 || m > (1 << 21) || n > (1 << 24)) return fail(OPEVO_E_ARG, "%s: %lld rows (at most 2^21) and %lld columns (at most 2^24)", who, (long long)m, (long long)n);
+    if (k < 1 || k > (1 << 24)) return fail(OPEVO_E_ARG, "%s: K = %lld (1 to 2^24)", who, (long long)k);
+    if (m == 0 || n == 0) return OPEVO_OK;
+    const int64_t bytes = (k + 1) / 2, blocks = (k + 31) / 32;
+    if (int rc = check_rows(who, "a", p.a, p.lda, bytes, 1)) return rc;
+    if (int rc = check_rows(who, "scale_a", p.sa, p.ldsa, blocks, 1)) return rc;
+    if (int rc = check_rows(who, "b", p.b, p.ldb, bytes, 1)) return rc;
+    if (int rc = check_rows(who, "scale_b", p.sb, p.ldsb, blocks, 1)) return rc;
+    if (int rc = check_rows(who, "c", p.c, p.ldc, n, size_of(p.out))) return rc;
+    p.m = m; p.n = (int)n; p.k = (int)bytes; p.blocks = (int)blocks; p.odd = k % 2 != 0; p.experts = experts;
+    return run_product4(p, static_cast<hipStream_t>(stream));
+}
+
+}  // namespace
+
+extern "C" int opevo_matmul_mx4(const uint8_t *a, int64_t lda, const uint8_t *scale_a, int64_t ld_scale_a, const uint8_t *b, int64_t ldb, const uint8_t *scale_b,
+                                int64_t ld_scale_b, void *c, int64_t ldc, int out_dtype, int64_t M, int64_t N, int64_t K, void *stream)
+{
+    Product4 p = {a, b, scale_a, scale_b, (long)lda, (long)ldb, (long)ld_scale_a, (long)ld_scale_b, nullptr, 0, c, (long)ldc, out_dtype, 0, 0, 0, 0, false};
+    return product4("matmul_mx4", p, M, N, K, 0, stream);
+}
+
+extern "C" int opevo_matmul_mx4_grouped(const uint8_t *a, int64_t lda, const uint8_t *scale_a, int64_t ld_scale_a, const uint8_t *b, int64_t ldb, const uint8_t *scale_b,
+                                        int64_t ld_scale_b, const int32_t *offsets, int experts, void *c, int64_t ldc, int out_dtype, int64_t rows, int64_t N, int64_t K,
+                                        void *stream)
+{
+    const char *who = "matmul_mx4_grouped";
+    if (experts < 1 || experts > OPEVO_ROUTE_MAX_EXPERTS) return fail(OPEVO_E_ARG, "%s: %d experts (1 to %d)", who, experts, OPEVO_ROUTE_MAX_EXPERTS);
+    if (rows > 0 && N > 0 && (!offsets || reinterpret_cast<uintptr_t>(offsets) % 4)) return fail(OPEVO_E_ARG, "%s: offsets is NULL or not aligned to 4 bytes", who);
+    Product4 p = {a, b, scale_a, scale_b, (long)lda, (long)ldb, (long)ld_scale_a, (long)ld_scale_b, offsets, experts, c, (long)ldc, out_dtype, 0, 0, 0, 0, false};
+    return product4(who, p, rows, N, K, experts, stream);
+}

@@ -1,0 +1,470 @@
+// RMS norm of rows with the residual's addition in front of it, its rows in 8 bits, and its gradient:
+//   s = round(x + r),  i = 1 / sqrt(mean(s^2) + eps),  y = s i w,
+//   dx = i (w dy - s i^2 mean(w dy s)) + ds,  dw = sum over rows of dy s i.
+// Bound by memory: a row is read once, held in registers while its sum of squares is formed, and written from there.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cfloat>
+#include <cstdint>
+
+#include "launch.hpp"
+#include "narrow.hpp"
+#include "rows.hpp"
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// A row's pieces of 16 bytes.  The last one may be short and is then taken element by element: no element belongs to two pieces, so a lane may write where it has read
+// (a sum in place of the residual) whatever other lanes have still to read.
+template <typename T> struct Row {
+    static constexpr int n = Vec<T>::n;
+    int width, count;
+    __device__ explicit Row(int w) : width(w), count((w + n - 1) / n) {}
+    __device__ __forceinline__ Vec<T> load(const T *row, int i) const
+    {
+        Vec<T> v = {};
+        if (i * n + n <= width) __builtin_memcpy(&v, row + i * n, 16);
+        else
+#pragma unroll
+            for (int e = 0; e < n; ++e)
+                if (i * n + e < width) v.v[e] = row[i * n + e];
+        return v;
+    }
+    template <typename O> __device__ __forceinline__ void store(O *row, int i, const O (&v)[n]) const
+    {
+        if (i * n + n <= width) __builtin_memcpy(row + i * n, v, sizeof v);
+        else
+#pragma unroll
+            for (int e = 0; e < n; ++e)
+                if (i * n + e < width) row[i * n + e] = v[e];
+    }
+};
+
+// Lanes of a row: `tx` side by side, a power of two.  What they hold is combined in an order that depends on tx alone.
+template <typename V, typename F>
+__device__ __forceinline__ V of_row(V v, int tx, V (&red)[kThreads / 64], F &&f)
+{
+    for (int o = 1; o < tx && o < 64; o <<= 1) v = f(v, (V)__shfl_xor(v, o));
+    if (tx > 64) {                          // alike for the whole workgroup
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+        __syncthreads();
+        const int w0 = (int)((threadIdx.x >> __builtin_ctz(tx)) << (__builtin_ctz(tx) - 6));
+        v = red[w0];
+        for (int w = 1; w < tx / 64; ++w) v = f(v, red[w0 + w]);
+    }
+    return v;
+}
+
+// s w as the quantiser takes it: without rounding.  The product of two bf16 has 16 bits and that of two fp16 22, so fp32 holds it; fp32's takes 48 and goes into fp64.
+template <typename T> struct Exact { typedef float type; };
+template <> struct Exact<float> { typedef double type; };
+
+// q = round(127 v / a).  v times 127 / a in fp32 is off by at most three roundings, 127 * 3 * 2^-24 = 2.3e-5, and rounds to the same integer unless it is within 4e-5 of
+// the middle between two; then the quotient is formed in fp64, where the middle is hit only by quotients that are there.
+template <typename V> struct RowTo8 {
+    V a;
+    float inv, pre;
+    bool on;
+    __device__ explicit RowTo8(V a_) : a(a_)
+    {
+        pre = a > (V)1e30 ? 0x1p-96f : a < (V)1e-30 ? 0x1p96f : 1.f;        // neither the factor nor its product overflows
+        inv = 127.f / (float)(a * (V)pre);
+        on = a > 0 && a <= (V)FLT_MAX;
+    }
+    __device__ __forceinline__ int8_t operator()(V v) const
+    {
+        constexpr float kRound = 12582912.f;                // 1.5 * 2^23: what is added to it is rounded to an integer, in its low bits
+        const float f = (float)(v * (V)pre), r = fmaf(f, inv, kRound);
+        int q = (int)(__float_as_uint(r) & 0xff);
+        if (fabsf(fmaf(f, inv, kRound - r)) > 0.49996f) q = (int)rint(127.0 * (double)v / (double)a);
+        return (int8_t)(on ? q : 0);
+    }
+};
+
+struct Norm {
+    const void *x, *residual, *weight;
+    long ld_x, ld_residual;
+    void *sum;
+    long ld_sum;
+    void *y;                // the norm in the rows' type, or in 8 bits
+    long ld_y;
+    float *per_row;         // 1 / rms, or the scale of a row in 8 bits; may be NULL in the first case
+    long rows;
+    int width, tx;
+    float eps;
+};
+
+template <typename T, int HOLD, bool TO8>
+__global__ __launch_bounds__(kThreads)
+void norm_rows(Norm p)
+{
+    typedef typename Exact<T>::type V;
+    constexpr int n = Vec<T>::n;
+    __shared__ float red[kThreads / 64];
+    __shared__ V red8[kThreads / 64];
+    const int tx = p.tx, lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx);
+    const long row = this_block() * ty + ((int)threadIdx.x >> __builtin_ctz(tx));
+    const bool on = row < p.rows;
+    const Row<T> at(on ? p.width : 0);
+    const T *x = (const T *)p.x + row * p.ld_x, *r = (const T *)p.residual + row * p.ld_residual, *w = (const T *)p.weight;
+    auto summed = [&](int i) {
+        Vec<T> s = at.load(x, i);
+        if (p.residual) {
+            const Vec<T> add = at.load(r, i);
+#pragma unroll
+            for (int e = 0; e < n; ++e) s.v[e] = narrow<T>((float)s.v[e] + (float)add.v[e]);
+        }
+        return s;
+    };
+    auto weights = [&](int i) {
+        if (w) return at.load(w, i);
+        Vec<T> one;
+#pragma unroll
+        for (int e = 0; e < n; ++e) one.v[e] = (T)1.f;
+        return one;
+    };
+    Vec<T> s[HOLD], add[HOLD];
+#pragma unroll
+    for (int u = 0; u < HOLD; ++u) {
+        s[u] = {};
+        if (lane + u * tx < at.count) s[u] = at.load(x, lane + u * tx);
+    }
+    if (p.residual) {
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u) {
+            add[u] = {};
+            if (lane + u * tx < at.count) add[u] = at.load(r, lane + u * tx);
+        }
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u)
+#pragma unroll
+            for (int e = 0; e < n; ++e) s[u].v[e] = narrow<T>((float)s[u].v[e] + (float)add[u].v[e]);
+    }
+    float squares = 0.f;
+    V most = 0;
+    auto look = [&](int i, const Vec<T> &v) {
+#pragma unroll
+        for (int e = 0; e < n; ++e) squares = fmaf((float)v.v[e], (float)v.v[e], squares);
+        if (TO8) {
+            const Vec<T> by = weights(i);
+#pragma unroll
+            for (int e = 0; e < n; ++e) {
+                V m = fabs((V)v.v[e] * (V)by.v[e]);
+                if (!(m <= (V)FLT_MAX)) m = (V)INFINITY;    // NaN too: a maximum passes over it
+                most = fmax(most, m);
+            }
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < HOLD; ++u)
+        if (lane + u * tx < at.count) look(lane + u * tx, s[u]);
+    for (int i = lane + HOLD * tx; i < at.count; i += tx) look(i, summed(i));
+    squares = of_row(squares, tx, red, [](float a, float b) { return a + b; });
+    const float inv = 1.f / sqrtf(squares / (float)p.width + p.eps);
+    if (TO8) most = of_row(most, tx, red8, [](V a, V b) { return fmax(a, b); });
+    if (!on) return;
+    const RowTo8<V> to8(most);
+    T *sum = (T *)p.sum + row * p.ld_sum;
+    auto write = [&](int i, const Vec<T> &v) {
+        if (p.sum) at.store(sum, i, v.v);
+        const Vec<T> by = weights(i);
+        if constexpr (TO8) {
+            int8_t q[n];
+#pragma unroll
+            for (int e = 0; e < n; ++e) q[e] = to8((V)v.v[e] * (V)by.v[e]);
+            at.store((int8_t *)p.y + row * p.ld_y, i, q);
+        } else {
+            Vec<T> y;
+#pragma unroll
+            for (int e = 0; e < n; ++e) y.v[e] = narrow<T>((float)v.v[e] * inv * (float)by.v[e]);
+            at.store((T *)p.y + row * p.ld_y, i, y.v);
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < HOLD; ++u)
+        if (lane + u * tx < at.count) write(lane + u * tx, s[u]);
+    for (int i = lane + HOLD * tx; i < at.count; i += tx) write(i, summed(i));
+    if (lane == 0 && p.per_row) p.per_row[row] = !TO8 ? inv : most <= (V)FLT_MAX ? (float)(most * (V)inv / (V)127) : __uint_as_float(0x7fc00000u);
+}
+
+// ------------------------------------------------------------------ gradient
+struct Grad {
+    const void *dy, *dsum, *sum, *weight;
+    long ld_dy, ld_dsum, ld_sum;
+    const float *inv_rms;
+    void *dx;
+    long ld_dx;
+    float *dw;              // [workgroups][width] partial sums, or the gradient itself of one workgroup; NULL: not wanted
+    long rows;
+    int width, tx;
+};
+
+template <typename T, int HOLD>
+__global__ __launch_bounds__(kThreads)
+void norm_grad(Grad p)
+{
+    constexpr int n = Vec<T>::n;
+    __shared__ float red[2][kThreads / 64];
+    __shared__ float part[HOLD * kThreads * n];
+    const int tx = p.tx, lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx), line = (int)threadIdx.x >> __builtin_ctz(tx);
+    const Row<T> at(p.width);
+    const T *w = (const T *)p.weight;
+    auto weights = [&](int i) {
+        if (w) return at.load(w, i);
+        Vec<T> one;
+#pragma unroll
+        for (int e = 0; e < n; ++e) one.v[e] = (T)1.f;
+        return one;
+    };
+    Vec<T> by[HOLD];
+    float dw[HOLD][n] = {};
+#pragma unroll
+    for (int u = 0; u < HOLD; ++u) {
+        by[u] = {};
+        if (lane + u * tx < at.count) by[u] = weights(lane + u * tx);
+    }
+    float *own = p.dw ? p.dw + (long)blockIdx.x * p.width : nullptr;
+    const long step = (long)gridDim.x * ty;
+    Vec<T> g[HOLD], s[HOLD], next_g[HOLD], next_s[HOLD];
+    auto load = [&](Vec<T> (&g)[HOLD], Vec<T> (&s)[HOLD], long row) {
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u) {
+            g[u] = {};
+            s[u] = {};
+            if (row < p.rows && lane + u * tx < at.count) {
+                g[u] = at.load((const T *)p.dy + row * p.ld_dy, lane + u * tx);
+                s[u] = at.load((const T *)p.sum + row * p.ld_sum, lane + u * tx);
+            }
+        }
+    };
+    int turn = 0;
+    long row = (long)blockIdx.x * ty + line;
+    load(g, s, row);
+    // rows of a workgroup's lines in step: of_row meets all its threads
+    for (long row0 = (long)blockIdx.x * ty; row0 < p.rows; row0 += step, row += step, turn ^= 1) {
+        const bool on = row < p.rows;
+        const T *dy = (const T *)p.dy + row * p.ld_dy, *sum = (const T *)p.sum + row * p.ld_sum;
+        load(next_g, next_s, row + step);
+        const float inv = on ? p.inv_rms[row] : 0.f;
+        Vec<T> add[HOLD];
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u) {
+            add[u] = {};
+            if (p.dsum && on && lane + u * tx < at.count) add[u] = at.load((const T *)p.dsum + row * p.ld_dsum, lane + u * tx);
+        }
+        float dot = 0.f;
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u)
+#pragma unroll
+            for (int e = 0; e < n; ++e) dot = fmaf((float)by[u].v[e] * (float)g[u].v[e], (float)s[u].v[e], dot);
+        for (int i = lane + HOLD * tx; on && i < at.count; i += tx) {
+            const Vec<T> gi = at.load(dy, i), si = at.load(sum, i), wi = weights(i);
+#pragma unroll
+            for (int e = 0; e < n; ++e) dot = fmaf((float)wi.v[e] * (float)gi.v[e], (float)si.v[e], dot);
+        }
+        dot = of_row(dot, tx, red[turn], [](float a, float b) { return a + b; });
+        const float back = inv * inv * (dot / (float)p.width);
+        auto write = [&](int i, const Vec<T> &gi, const Vec<T> &si, const Vec<T> &wi, const Vec<T> &ai) {
+            Vec<T> out;
+#pragma unroll
+            for (int e = 0; e < n; ++e) {
+                const float v = inv * ((float)wi.v[e] * (float)gi.v[e] - (float)si.v[e] * back);
+                out.v[e] = narrow<T>(p.dsum ? v + (float)ai.v[e] : v);
+            }
+            at.store((T *)p.dx + row * p.ld_dx, i, out.v);
+        };
+        if (on) {
+#pragma unroll
+            for (int u = 0; u < HOLD; ++u) {
+                if (lane + u * tx < at.count) write(lane + u * tx, g[u], s[u], by[u], add[u]);
+#pragma unroll
+                for (int e = 0; e < n; ++e) dw[u][e] = fmaf((float)g[u].v[e], (float)s[u].v[e] * inv, dw[u][e]);
+            }
+            // pieces that no lane holds: tx is the whole workgroup then (ty = 1), and their partial sums stay in memory, each a lane's own
+            for (int i = lane + HOLD * tx; i < at.count; i += tx) {
+                const Vec<T> gi = at.load(dy, i), si = at.load(sum, i), wi = weights(i);
+                Vec<T> ai = {};
+                if (p.dsum) ai = at.load((const T *)p.dsum + row * p.ld_dsum, i);
+                if (own)
+#pragma unroll
+                    for (int e = 0; e < n; ++e)
+                        if (i * n + e < p.width) own[i * n + e] = fmaf((float)gi.v[e], (float)si.v[e] * inv, row0 == (long)blockIdx.x ? 0.f : own[i * n + e]);
+                write(i, gi, si, wi, ai);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u) { g[u] = next_g[u]; s[u] = next_s[u]; }
+    }
+    if (!own) return;
+    // the lines' sums, one line after the other
+    for (int l = 0; l < ty; ++l) {
+        if (line == l)
+#pragma unroll
+            for (int u = 0; u < HOLD; ++u)
+#pragma unroll
+                for (int e = 0; e < n; ++e) {
+                    float &to = part[(e * HOLD + u) * tx + lane];
+                    to = l == 0 ? dw[u][e] : to + dw[u][e];
+                }
+        __syncthreads();
+    }
+    const int held = min(p.width, HOLD * tx * n);
+    for (int c = threadIdx.x; c < held; c += kThreads) {
+        const int i = c / n, u = i / tx;
+        own[c] = part[(c % n * HOLD + u) * tx + i - u * tx];
+    }
+    if (p.rows == 0)
+        for (int c = held + threadIdx.x; c < p.width; c += kThreads) own[c] = 0.f;
+}
+
+// dw[c] = the sum of part[0 .. parts][c]: kCols columns a workgroup, a part of the lines each thread, joined in the LDS.
+constexpr int kCols = 16, kLines = 64;
+__global__ __launch_bounds__(kCols * kLines)
+void norm_grad_weight(const float *__restrict__ part, int parts, int width, float *__restrict__ dw)
+{
+    __shared__ float red[kLines][kCols + 1];
+    const int col = (int)threadIdx.x % kCols, line = (int)threadIdx.x / kCols;
+    const long c = (long)blockIdx.x * kCols + col;
+    float sum = 0.f;
+    if (c < width)
+#pragma unroll 8
+        for (int i = line; i < parts; i += kLines) sum += part[(long)i * width + c];
+    red[line][col] = sum;
+    __syncthreads();
+    for (int half = kLines / 2; half > 0; half /= 2) {
+        if (line < half) red[line][col] += red[line + half][col];
+        __syncthreads();
+    }
+    if (line == 0 && c < width) dw[c] = red[0][col];
+}
+
+// ------------------------------------------------------------------ host side
+using opevo::launch;
+
+// `tx` lanes to a row of `pieces`, `hold` pieces a lane.
+struct Shape { int tx, hold; };
+Shape shape_of(int64_t pieces, int64_t rows, int most)
+{
+    int tx = 1, hold = 1;
+    while (tx < kThreads && tx < pieces) tx *= 2;
+    while (hold < most && (int64_t)tx * hold < pieces) hold *= 2;
+    while (tx > 64 && hold < most && rows * (tx / 2) / 64 >= 4096) { tx /= 2; hold *= 2; }
+    return {tx, hold};
+}
+
+int check_norm(const char *who, const Norm &p, int dtype, int64_t rows, int64_t width)
+{
+    if (!known(dtype)) return fail(OPEVO_E_ARG, "%s: unknown element type %d", who, dtype);
+    if (rows < 0 || rows > INT32_MAX) return fail(OPEVO_E_ARG, "%s: %lld rows", who, (long long)rows);
+    if (!(p.eps >= 0.f) || p.eps > FLT_MAX) return fail(OPEVO_E_ARG, "%s: eps is negative, infinite or not a number", who);
+    if (rows == 0) return OPEVO_OK;
+    const size_t size = size_of(dtype);
+    if (int rc = check_rows(who, "x", p.x, p.ld_x, width, size)) return rc;
+    if (p.residual)
+        if (int rc = check_rows(who, "residual", p.residual, p.ld_residual, width, size)) return rc;
+    if (p.residual && !p.sum) return fail(OPEVO_E_ARG, "%s: sum is NULL, but there is a residual", who);
+    if (p.sum)
+        if (int rc = check_rows(who, "sum", p.sum, p.ld_sum, width, size)) return rc;
+    if (!aligned(p.weight, size)) return fail(OPEVO_E_ARG, "%s: weight is not aligned to its elements", who);
+    return OPEVO_OK;
+}
+
+template <typename T, bool TO8>
+int run_norm(Norm p, hipStream_t stream)
+{
+    const Shape l = shape_of((p.width + Vec<T>::n - 1) / Vec<T>::n, p.rows, 8);
+    p.tx = l.tx;
+    const int ty = kThreads / l.tx;
+    auto *k = l.hold == 1 ? norm_rows<T, 1, TO8> : l.hold == 2 ? norm_rows<T, 2, TO8> : l.hold == 4 ? norm_rows<T, 4, TO8> : norm_rows<T, 8, TO8>;
+    return launch("norm_rows launch", k, spread((p.rows + ty - 1) / ty), dim3(kThreads), stream, p);
+}
+template <typename T> int run_plain(const Norm &p, hipStream_t stream) { return run_norm<T, false>(p, stream); }
+template <typename T> int run_to8(const Norm &p, hipStream_t stream) { return run_norm<T, true>(p, stream); }
+
+// Workgroups of the gradient: each goes through its rows with the weight's gradient in registers.
+constexpr int64_t kGroups = 512;
+int64_t groups_of(int64_t rows, int ty) { return std::max<int64_t>(1, std::min<int64_t>(kGroups, (rows + ty - 1) / ty)); }
+
+template <typename T>
+int run_grad(Grad p, float *dweight, float *workspace, hipStream_t stream)
+{
+    const Shape l = shape_of((p.width + Vec<T>::n - 1) / Vec<T>::n, 1, 4);
+    p.tx = l.tx;
+    const int64_t groups = groups_of(p.rows, kThreads / l.tx);
+    p.dw = !dweight ? nullptr : groups == 1 ? dweight : workspace;
+    auto *k = l.hold == 1 ? norm_grad<T, 1> : l.hold == 2 ? norm_grad<T, 2> : norm_grad<T, 4>;
+    if (int rc = launch("norm_grad launch", k, dim3((unsigned)groups), dim3(kThreads), stream, p)) return rc;
+    if (!dweight || groups == 1) return OPEVO_OK;
+    return launch("norm_grad_weight launch", norm_grad_weight, dim3((p.width + kCols - 1) / kCols), dim3(kCols * kLines), stream, workspace, (int)groups, p.width, dweight);
+}
+
+}  // namespace
+
+extern "C" int opevo_norm_rows(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual, const void *weight, float eps, int dtype, int64_t rows,
+                               int64_t width, void *sum, int64_t ld_sum, void *y, int64_t ld_y, float *inv_rms, void *stream)
+{
+    const char *who = "norm_rows";
+    Norm p = {x, residual, weight, (long)ld_x, (long)ld_residual, sum, (long)ld_sum, y, (long)ld_y, inv_rms, (long)rows, (int)width, 0, eps};
+    if (int rc = check_norm(who, p, dtype, rows, width)) return rc;
+    if (rows == 0) return OPEVO_OK;
+    if (int rc = check_rows(who, "y", y, ld_y, width, size_of(dtype))) return rc;
+    if (!aligned(inv_rms, 4)) return fail(OPEVO_E_ARG, "%s: inv_rms is not aligned to 4 bytes", who);
+    return BY_DTYPE(dtype, run_plain, p, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int opevo_norm_rows_i8(const void *x, int64_t ld_x, const void *residual, int64_t ld_residual, const void *weight, float eps, int dtype, int64_t rows,
+                                  int64_t width, void *sum, int64_t ld_sum, int8_t *q, int64_t ld_q, float *scale, void *stream)
+{
+    const char *who = "norm_rows_i8";
+    Norm p = {x, residual, weight, (long)ld_x, (long)ld_residual, sum, (long)ld_sum, q, (long)ld_q, scale, (long)rows, (int)width, 0, eps};
+    if (int rc = check_norm(who, p, dtype, rows, width)) return rc;
+    if (rows == 0) return OPEVO_OK;
+    if (int rc = check_rows(who, "q", q, ld_q, width, 1)) return rc;
+    if (int rc = check_words(who, "scale", scale)) return rc;
+    return BY_DTYPE(dtype, run_to8, p, static_cast<hipStream_t>(stream));
+}
+
+static int check_size(const char *who, int64_t rows, int64_t width)
+{
+    if (rows < 0 || rows > INT32_MAX) return fail(OPEVO_E_ARG, "%s: %lld rows", who, (long long)rows);
+    if (width < 1 || width > (1 << 24)) return fail(OPEVO_E_ARG, "%s: rows of %lld elements (1 to 2^24)", who, (long long)width);
+    return OPEVO_OK;
+}
+
+extern "C" int opevo_norm_rows_grad_workspace(int64_t rows, int64_t width, size_t *bytes)
+{
+    if (!bytes) return fail(OPEVO_E_ARG, "norm_rows_grad_workspace: bytes is NULL");
+    if (int rc = check_size("norm_rows_grad_workspace", rows, width)) return rc;
+    const int64_t groups = std::min(kGroups, rows);
+    *bytes = groups <= 1 ? 0 : sizeof(float) * (size_t)(groups * width);
+    return OPEVO_OK;
+}
+
+extern "C" int opevo_norm_rows_grad(const void *dy, int64_t ld_dy, const void *dsum, int64_t ld_dsum, const void *sum, int64_t ld_sum, const void *weight,
+                                    const float *inv_rms, int dtype, int64_t rows, int64_t width, void *dx, int64_t ld_dx, float *dweight, void *workspace,
+                                    size_t workspace_bytes, void *stream)
+{
+    const char *who = "norm_rows_grad";
+    if (!known(dtype)) return fail(OPEVO_E_ARG, "%s: unknown element type %d", who, dtype);
+    if (int rc = check_size(who, rows, width)) return rc;
+    const size_t size = size_of(dtype);
+    if (dweight && !aligned(dweight, 4)) return fail(OPEVO_E_ARG, "%s: dweight is not aligned to 4 bytes", who);
+    if (rows > 0) {
+        if (int rc = check_rows(who, "dy", dy, ld_dy, width, size)) return rc;
+        if (dsum)
+            if (int rc = check_rows(who, "dsum", dsum, ld_dsum, width, size)) return rc;
+        if (int rc = check_rows(who, "sum", sum, ld_sum, width, size)) return rc;
+        if (int rc = check_rows(who, "dx", dx, ld_dx, width, size)) return rc;
+        if (int rc = check_words(who, "inv_rms", inv_rms)) return rc;
+        if (!aligned(weight, size)) return fail(OPEVO_E_ARG, "%s: weight is not aligned to its elements", who);
+    }
+    size_t need = 0;
+    if (int rc = opevo_norm_rows_grad_workspace(rows, width, &need)) return rc;
+    if (dweight && need && (!workspace || !aligned(workspace, 4) || workspace_bytes < need))
+        return fail(OPEVO_E_ARG, "%s: the workspace holds %zu bytes of the %zu it takes, or is not aligned to 4 bytes", who, workspace ? workspace_bytes : 0, need);
+    if (rows == 0 && !dweight) return OPEVO_OK;
+    Grad p = {dy, dsum, sum, weight, (long)ld_dy, (long)ld_dsum, (long)ld_sum, inv_rms, dx, (long)ld_dx, nullptr, (long)rows, (int)width, 0};
+    return BY_DTYPE(dtype, run_grad, p, dweight, static_cast<float *>(workspace), static_cast<hipStream_t>(stream));
+}
