@@ -562,6 +562,24 @@ int opevo_matmul_mx4_grouped(const uint8_t *a, int64_t lda, const uint8_t *scale
                              int64_t ld_scale_b, const int32_t *offsets, int experts, void *c, int64_t ldc, int out_dtype, int64_t rows, int64_t N,
                              int64_t K, void *stream);
 
+/* A whole layer of experts for few tokens, in two launches: for every slot s = (t, j) of an expert e that is held here
+ *   h = silu(x[t] Wg[e]^T) * (x[t] Wu[e]^T),   y[t] = sum over j of weight[s] * (h Wo[e]^T)
+ * with silu(g) = g / (1 + exp(-g)).  x and y [tokens][width] in dtype; expert and weight (fp32, or NULL: 1) [tokens * k] as opevo_route_dispatch and opevo_route_combine take them: a slot
+ * whose id is outside [0, experts) adds nothing, whatever its weight, and a token without any other gets zeros.  w_in [experts][2 * inner][width]: the rows of Wg before those of Wu; w_out
+ * [experts][width][inner]; all rows of either ld_* apart.  Weights in 8 bits with a scale for each row (scale_in [experts][2 * inner], scale_out [experts][width]), or in microscaled
+ * 4 bits along their rows.  Activations are not quantised: x is taken as it is, h is kept to 2^-16 of its value (fp32 callers: as it is), sums are fp32, and y is rounded once.  tokens * k at
+ * most OPEVO_EXPERT_LAYER_MAX_SLOTS (more: opevo_route_dispatch and the products by expert), width and inner at most 2^20. */
+#define OPEVO_EXPERT_LAYER_MAX_SLOTS 512
+/* Bytes of workspace (16-byte aligned) that a layer of this size takes.  Host only. */
+int opevo_expert_layer_workspace(int64_t tokens, int k, int dtype, int64_t inner, size_t *bytes);
+int opevo_expert_layer_i8(const void *x, int64_t ld_x, int dtype, const int32_t *expert, const float *weight, int64_t tokens, int k, int experts,
+                          int64_t width, int64_t inner, const int8_t *w_in, int64_t ld_in, const float *scale_in, const int8_t *w_out, int64_t ld_out,
+                          const float *scale_out, void *y, int64_t ld_y, void *workspace, size_t workspace_bytes, void *stream);
+int opevo_expert_layer_mx4(const void *x, int64_t ld_x, int dtype, const int32_t *expert, const float *weight, int64_t tokens, int k, int experts,
+                           int64_t width, int64_t inner, const uint8_t *w_in, int64_t ld_in, const uint8_t *scale_in, int64_t ld_scale_in,
+                           const uint8_t *w_out, int64_t ld_out, const uint8_t *scale_out, int64_t ld_scale_out, void *y, int64_t ld_y, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
 /* -------------------------------------------------------- whole tuning run (Alg. 1) */
 typedef struct {
     const void *a, *b;         /* DEVICE inputs                                                  */

@@ -155,6 +155,10 @@ _SIGNATURES = {
     "opevo_dequantize_rows_mx4": [_vp, C.c_int64, _vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int64, _vp],
     "opevo_matmul_mx4": [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_int64, _vp],
     "opevo_matmul_mx4_grouped": [_vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int, _vp, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_int64, _vp],
+    "opevo_expert_layer_workspace": [C.c_int64, C.c_int, C.c_int, C.c_int64, C.POINTER(C.c_size_t)],
+    "opevo_expert_layer_i8": [_vp, C.c_int64, C.c_int, _vp, _vp, C.c_int64, C.c_int, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, C.c_int64, _vp, C.c_size_t, _vp],
+    "opevo_expert_layer_mx4": [_vp, C.c_int64, C.c_int, _vp, _vp, C.c_int64, C.c_int, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int64,
+                               _vp, C.c_size_t, _vp],
     "opevo_tune": [_vp, C.c_int, C.POINTER(opevo_tune_args), _i32p, C.POINTER(opevo_tune_result)],
 }
 for _name, _argtypes in _SIGNATURES.items():
@@ -662,6 +666,25 @@ def opevo_matmul_mx4_grouped(a: int, lda: int, scale_a: int, ld_scale_a: int, b:
                              c: int, ldc: int, out_dtype: int, rows: int, N: int, K: int, stream: int = 0) -> None:
     """rows: how many rows A and C have; which expert a row belongs to stands in offsets, on the device."""
     _check(lib.opevo_matmul_mx4_grouped(a, lda, scale_a, ld_scale_a, b, ldb, scale_b, ld_scale_b, offsets, experts, c, ldc, out_dtype, rows, N, K, stream))
+
+
+def opevo_expert_layer_workspace(tokens: int, k: int, dtype: int, inner: int) -> int:
+    v = C.c_size_t()
+    _check(lib.opevo_expert_layer_workspace(tokens, k, dtype, inner, C.byref(v)))
+    return v.value
+
+
+def opevo_expert_layer_i8(x: int, ld_x: int, dtype: int, expert: int, weight: int, tokens: int, k: int, experts: int, width: int, inner: int, w_in: int, ld_in: int,
+                          scale_in: int, w_out: int, ld_out: int, scale_out: int, y: int, ld_y: int, workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(lib.opevo_expert_layer_i8(x, ld_x, dtype, expert, weight, tokens, k, experts, width, inner, w_in, ld_in, scale_in, w_out, ld_out, scale_out, y, ld_y, workspace,
+                                     workspace_bytes, stream))
+
+
+def opevo_expert_layer_mx4(x: int, ld_x: int, dtype: int, expert: int, weight: int, tokens: int, k: int, experts: int, width: int, inner: int, w_in: int, ld_in: int,
+                           scale_in: int, ld_scale_in: int, w_out: int, ld_out: int, scale_out: int, ld_scale_out: int, y: int, ld_y: int, workspace: int,
+                           workspace_bytes: int, stream: int = 0) -> None:
+    _check(lib.opevo_expert_layer_mx4(x, ld_x, dtype, expert, weight, tokens, k, experts, width, inner, w_in, ld_in, scale_in, ld_scale_in, w_out, ld_out, scale_out, ld_scale_out,
+                                      y, ld_y, workspace, workspace_bytes, stream))
 
 
 def opevo_tune(op, variant: int, a: int, b: int, c: int, ref: Optional[int] = None, stream: int = 0,

@@ -1,0 +1,517 @@
+// A whole layer of experts for few tokens, in two launches:
+//   h[s] = silu(x[t] Wg[e]^T) * (x[t] Wu[e]^T) for every slot s = (t, j) of expert e,   y[t] = sum_j weight[s] * (h[s] Wo[e]^T),
+// weights in 8 bits with a scale a channel or in microscaled 4 bits (mx4.hpp), activations as they are.  What bounds it are the weights of the experts in use, each of which is read once; the
+// products go through bf16 matrix instructions because those hold 8-bit integers and E2M1 values under their factors exactly.
+//
+// Activations of more bits go as a sum of bf16 numbers, each in a row of the product of its own: fp16 is the sum of two, fp32 of three, exactly, and h, which is fp32, is kept as two (an error of
+// 2^-16; three for fp32 callers).  The product has 16 rows whatever they hold, so for the few rows of an expert the parts cost nothing, and the rows' sums are added at the end.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "launch.hpp"
+#include "mx4.hpp"
+#include "narrow.hpp"
+#include "product.hpp"
+#include "rows.hpp"
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kMaxSlots = OPEVO_EXPERT_LAYER_MAX_SLOTS;
+constexpr int kWords = OPEVO_ROUTE_MAX_EXPERTS / 32;
+constexpr int kStep = 128;              // values along K of four matrix instructions; lane (r, g) holds those from 32 g on of row r
+
+// What the first launch leaves for the second: the experts in use in ascending order, where each one's rows of h start (rows are the held slots, sorted by expert), and every slot's row or -1.
+struct Plan {
+    int active, held, pad[2];
+    int expert[kMaxSlots], start[kMaxSlots], row[kMaxSlots];
+};
+
+struct Layer {
+    const void *x;
+    long ld_x;
+    const int *expert;
+    const float *weight;
+    int tokens, k, slots, experts, width, inner;
+    const uint8_t *win, *wout;
+    const void *sin, *sout;             // a float a channel, or a byte for 32 values
+    long ld_in, ld_out, ld_sin, ld_sout;
+    void *y;
+    long ld_y;
+    Plan *plan;
+    __bf16 *h;                          // [held slots][parts][ld_h]
+    long ld_h;
+};
+
+// The high halves of two fp32 numbers: both as bf16, towards zero.
+__device__ __forceinline__ int high_halves(float a, float b) { return (int)__builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
+// What is left of a number without its first eight bits; of an infinity nothing.
+__device__ __forceinline__ float rest(float v)
+{
+    const float high = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+    return v == high ? 0.f : v - high;
+}
+
+// ------------------------------------------------------------------ weights
+// Rows of weights, 16 of them to a tile: a lane has its row's pointer, loads 32 bytes of an iteration and makes of them the operands of SUB * 4 matrix instructions.
+struct Weights8 {
+    static constexpr int SUB = 1;
+    struct Raw { i32x4 v[2]; };
+    const uint8_t *row;
+    int k;
+    __device__ __forceinline__ void at(const uint8_t *w, long ld, const void *, long, long n, int k_) { row = w + n * ld; k = k_; }
+    __device__ __forceinline__ void load(Raw &r, int k0, int g) const
+    {
+        __builtin_memcpy(&r.v[0], row + k0 + g * 32, 16);
+        __builtin_memcpy(&r.v[1], row + k0 + g * 32 + 16, 16);
+    }
+    __device__ __forceinline__ void load_ragged(Raw &r, int k0, int g) const
+    {
+        r.v[0] = load_chunk((const int8_t *)row, k0 + g * 32, k);
+        r.v[1] = load_chunk((const int8_t *)row, k0 + g * 32 + 16, k);
+    }
+    static __device__ __forceinline__ bf16x8 operand(const Raw &r, int, int j, int)
+    {
+        i32x4 out;
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+            const int w = r.v[j / 2][j % 2 * 2 + d];
+            out[d * 2] = high_halves((float)(int8_t)w, (float)(int8_t)(w >> 8));
+            out[d * 2 + 1] = high_halves((float)(int8_t)(w >> 16), (float)(w >> 24));
+        }
+        return __builtin_bit_cast(bf16x8, out);
+    }
+    static __device__ __forceinline__ float scale(const void *s, long channel) { return ((const float *)s)[channel]; }
+};
+struct Weights4 {
+    static constexpr int SUB = 2;
+    struct Raw { i32x4 v[2]; i32x2 f; };
+    const uint8_t *row, *by;
+    int k;                              // values
+    __device__ __forceinline__ void at(const uint8_t *w, long ld, const void *s, long ld_s, long n, int k_) { row = w + n * ld; by = (const uint8_t *)s + n * ld_s; k = k_; }
+    __device__ __forceinline__ void load(Raw &r, int k0, int g) const
+    {
+        __builtin_memcpy(&r.f, by + k0 / 32, 8);
+        __builtin_memcpy(&r.v[0], row + k0 / 2 + g * 16, 16);
+        __builtin_memcpy(&r.v[1], row + k0 / 2 + g * 16 + kStep / 2, 16);
+    }
+    __device__ __forceinline__ void load_ragged(Raw &r, int k0, int g) const
+    {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            r.f[u] = load_factors(by, k0 / 32 + u * 4, (k + 31) / 32);
+            r.v[u] = load_codes(row, k0 / 2 + g * 16 + u * (kStep / 2), (k + 1) / 2, k % 2 != 0);
+        }
+    }
+    static __device__ __forceinline__ bf16x8 operand(const Raw &r, int u, int j, int g)
+    {
+        const int w = r.v[u][j];
+        const float by = mx4_factor((int)((unsigned)r.f[u] >> 8 * g & 255));
+        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, by, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, by, 1),
+                     c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, by, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, by, 3);
+        return bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+    }
+    static __device__ __forceinline__ float scale(const void *, long) { return 1.f; }
+};
+
+// ------------------------------------------------------------------ activations
+// How many bf16 numbers make one of a type, and what a row that holds the part `part` gives to the product.
+template <typename T> struct Parts { static constexpr int n = 1, h = 2; };
+template <> struct Parts<_Float16> { static constexpr int n = 2, h = 2; };
+template <> struct Parts<float> { static constexpr int n = 3, h = 3; };
+
+template <typename T> __device__ __forceinline__ bf16x8 operand(const T (&v)[8], int part)
+{
+    if constexpr (Parts<T>::n == 1) {
+        bf16x8 out;
+        __builtin_memcpy(&out, v, 16);
+        return out;
+    } else {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            f[i] = (float)v[i];
+            const float second = rest(f[i]);
+            if constexpr (Parts<T>::n == 2) f[i] = part == 0 ? f[i] : second;
+            else f[i] = part == 0 ? f[i] : part == 1 ? second : rest(second);
+        }
+        const i32x4 out = {high_halves(f[0], f[1]), high_halves(f[2], f[3]), high_halves(f[4], f[5]), high_halves(f[6], f[7])};
+        return __builtin_bit_cast(bf16x8, out);
+    }
+}
+
+// A lane's row of activations.  A lane without one takes any: a column of the product is its row's alone.
+template <typename T, int SUB> struct Activations {
+    struct Raw { T v[SUB][4][8]; };
+    const T *row;
+    int part, k;
+    __device__ __forceinline__ void load(Raw &r, int k0, int g) const
+    {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) __builtin_memcpy(r.v[u][j], row + k0 + u * kStep + g * 32 + j * 8, sizeof r.v[u][j]);
+    }
+    __device__ __forceinline__ void load_ragged(Raw &r, int k0, int g) const
+    {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                constexpr int size = sizeof(T), pieces = size / 2;
+                i32x4 part[pieces];
+#pragma unroll
+                for (int o = 0; o < pieces; ++o) part[o] = load_chunk((const int8_t *)row, (k0 + u * kStep + g * 32 + j * 8) * size + o * 16, k * size);
+                __builtin_memcpy(r.v[u][j], part, sizeof part);
+            }
+    }
+};
+
+// The iterations first, first + stride, ... along K, the last one of which may be ragged; the wave whose turn it is takes that one.  The weights of the next iteration come from memory meanwhile; the
+// activations, of the same one, from the caches: they are asked for first, because loads are waited for in their order.
+template <bool RAGGED, typename Q, typename T, int NI>
+__device__ __forceinline__ void multiply(const Q (&w)[NI], const Activations<T, Q::SUB> &x, int first, int stride, int g, f32x4 (&acc)[NI])
+{
+    constexpr int LONG = Q::SUB * kStep;
+    typedef typename Q::Raw W;
+    typedef typename Activations<T, Q::SUB>::Raw X;
+    const int whole = x.k / LONG;
+    auto load = [&](W (&wr)[NI], int it) {
+#pragma unroll
+        for (int n = 0; n < NI; ++n) w[n].load(wr[n], it * LONG, g);
+    };
+    auto use = [&](const W (&wr)[NI], const X &xr) {
+#pragma unroll
+        for (int u = 0; u < Q::SUB; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bf16x8 a = operand(xr.v[u][j], x.part);
+#pragma unroll
+                for (int n = 0; n < NI; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Q::operand(wr[n], u, j, g), a, acc[n], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);      // operands are made as they are used: all at once they would take all registers
+            }
+        // The sums are due: else the compiler moves their products behind the next branch, with all their operands.
+#pragma unroll
+        for (int n = 0; n < NI; ++n) asm volatile("" : "+v"(acc[n]));
+    };
+    auto step = [&](const W (&wr)[NI], W (&next)[NI], int it) {
+        X xr;
+        x.load(xr, it * LONG, g);
+        if (it + stride < whole) load(next, it + stride);
+        use(wr, xr);
+    };
+    W wa[NI], wb[NI];
+    int it = first;
+    if (it < whole) load(wa, it);
+    for (; it < whole; it += 2 * stride) {
+        step(wa, wb, it);
+        if (it + stride < whole) step(wb, wa, it + stride);
+    }
+    if (RAGGED && whole % stride == first) {
+        X xr;
+        x.load_ragged(xr, whole * LONG, g);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < NI; ++n) w[n].load_ragged(wa[n], whole * LONG, g);
+        use(wa, xr);
+    }
+}
+
+// ------------------------------------------------------------------ the first launch
+// The slots' experts, held ones as they are and others as -1, and a bit for every expert in use.
+template <int NT> __device__ __forceinline__ void read_slots(const Layer &p, int *ids, unsigned *words)
+{
+    if (threadIdx.x < kWords) words[threadIdx.x] = 0;
+    __syncthreads();
+    for (int s = threadIdx.x; s < p.slots; s += NT) {
+        const int e = p.expert[s];
+        const bool held = (unsigned)e < (unsigned)p.experts;
+        ids[s] = held ? e : -1;
+        if (held) atomicOr(&words[e >> 5], 1u << (e & 31));
+    }
+    __syncthreads();
+}
+
+// Written by one workgroup: a slot's row is the number of held slots of lower experts, plus the earlier ones of its own.
+template <int NT> __device__ __forceinline__ void write_plan(const Layer &p, const int *ids, const unsigned *words)
+{
+    int held = 0, active = 0;
+    for (int s = 0; s < p.slots; ++s) held += ids[s] >= 0;
+    for (int i = 0; i < kWords; ++i) active += __popc(words[i]);
+    if (threadIdx.x == 0) { p.plan->active = active; p.plan->held = held; }
+    for (int s = threadIdx.x; s < p.slots; s += NT) {
+        const int e = ids[s];
+        int before = 0, same = 0;
+        for (int o = 0; o < p.slots; ++o) {
+            const int other = ids[o];
+            before += other >= 0 && other < e;
+            same += o < s && other == e;
+        }
+        p.plan->row[s] = e < 0 ? -1 : before + same;
+        if (e >= 0 && same == 0) {              // the first one of its expert
+            int index = __popc(words[e >> 5] & ((1u << (e & 31)) - 1u));
+            for (int i = 0; i < e >> 5; ++i) index += __popc(words[i]);
+            p.plan->expert[index] = e;
+            p.plan->start[index] = before;
+        }
+    }
+}
+
+// The expert number `index` of those in use, or -1.
+__device__ __forceinline__ int expert_at(const unsigned *words, int index, int lane)
+{
+    const unsigned w = lane < kWords ? words[lane] : 0;
+    const int n = __popc(w);
+    int sum = n;
+#pragma unroll
+    for (int o = 1; o < kWords; o <<= 1) {
+        const int up = __shfl_up(sum, o);
+        if (lane >= o) sum += up;
+    }
+    const unsigned long long past = __ballot(lane < kWords && sum > index);
+    if (!past) return -1;
+    const int at = __ffsll(past) - 1;
+    unsigned left = (unsigned)__builtin_amdgcn_readlane((int)w, at);
+    for (int skip = index - __builtin_amdgcn_readlane(sum - n, at); skip > 0; --skip) left &= left - 1;
+    return at * 32 + __ffs(left) - 1;
+}
+
+// h of an expert's rows for 16 * NP of its inner channels: gate and up, NP tiles of 16 rows of weights each.  The W waves deal the iterations along K among themselves.  NP is 2, so that the operands of
+// the activations serve four tiles, and 1 where K ends inside an iteration: the ragged loads would not leave registers for more.
+template <typename T, typename Q, int W, bool RAGGED>
+__global__ __launch_bounds__(W * 64, 2)
+void layer_in(Layer p)
+{
+    constexpr int NT = W * 64, NP = RAGGED ? 1 : 2, NI = 2 * NP, PX = Parts<T>::n, PH = Parts<T>::h, PER = 16 / PX;
+    __shared__ int ids[kMaxSlots], list[kMaxSlots];
+    __shared__ unsigned words[kWords];
+    __shared__ f32x4 sums[W][NI][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
+    read_slots<NT>(p, ids, words);
+    if (blockIdx.y == gridDim.y - 1) {
+        if (blockIdx.x == 0) write_plan<NT>(p, ids, words);
+        return;
+    }
+    const int e = expert_at(words, blockIdx.y, lane);
+    if (e < 0) return;                      // alike for the workgroup
+    int base = 0, rows = 0;
+    for (int s0 = 0; s0 < p.slots; s0 += 64) {
+        const int id = s0 + lane < p.slots ? ids[s0 + lane] : -1;
+        const unsigned long long same = __ballot(id == e);
+        if (wave == 0 && id == e) list[rows + __popcll(same & ((1ull << lane) - 1ull))] = s0 + lane;
+        base += __popcll(__ballot(id >= 0 && id < e));
+        rows += __popcll(same);
+    }
+    __syncthreads();
+    const int c0 = blockIdx.x * (NP * 16);
+    const long first = (long)e * 2 * p.inner;
+    Q w[NI];
+#pragma unroll
+    for (int n = 0; n < NI; ++n) w[n].at(p.win, p.ld_in, p.sin, p.ld_sin, first + (n < NP ? 0 : p.inner) + min(c0 + n % NP * 16 + r, p.inner - 1), p.width);
+    for (int t0 = 0; t0 < rows; t0 += PER) {
+        Activations<T, Q::SUB> x;
+        x.row = (const T *)p.x + list[min(t0 + r / PX, rows - 1)] / p.k * p.ld_x;
+        x.part = r % PX;
+        x.k = p.width;
+        f32x4 acc[NI] = {};
+        multiply<RAGGED, Q, T, NI>(w, x, wave, W, g, acc);
+#pragma unroll
+        for (int n = 0; n < NI; ++n) sums[wave][n][lane] = acc[n];
+        __syncthreads();
+        // an output a thread: one inner channel of one row
+        for (int o = threadIdx.x; o < PER * NP * 16; o += NT) {
+            const int c = o % (NP * 16), at = o / (NP * 16), row = t0 + at;
+            if (row >= rows || c0 + c >= p.inner) continue;
+            float v[2] = {0.f, 0.f};
+#pragma unroll
+            for (int side = 0; side < 2; ++side)
+#pragma unroll
+                for (int part = PX - 1; part >= 0; --part)
+                    for (int o = 0; o < W; ++o) v[side] += ((const float *)&sums[o][side * NP + c / 16][c % 16 / 4 * 16 + at * PX + part])[c % 4];
+            const float gate = v[0] * Q::scale(p.sin, first + c0 + c), up = v[1] * Q::scale(p.sin, first + p.inner + c0 + c);
+            const float h = gate / (1.f + expf(-gate)) * up, second = rest(h);
+            __bf16 *to = p.h + (long)(base + row) * PH * p.ld_h + c0 + c;
+            to[0] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(h) >> 16));
+            if constexpr (PH == 2) to[p.ld_h] = (__bf16)second;
+            else {
+                to[p.ld_h] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(second) >> 16));
+                to[2 * p.ld_h] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(rest(second)) >> 16));
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ the second launch
+// y of 16 columns for all tokens: a task is an expert in use and a share of K, the W waves deal the tasks among themselves, what they find for each row meets in LDS, and the rows of a
+// token are added up there in the order of its slots.
+constexpr int kShares = 1024;           // rows of 16 sums in the LDS
+
+template <typename T, typename Q, int W, bool RAGGED>
+__global__ __launch_bounds__(W * 64)
+void layer_out(Layer p)
+{
+    constexpr int NT = W * 64, PH = Parts<T>::h, PER = 16 / PH;
+    __shared__ int expert[kMaxSlots], start[kMaxSlots + 1], place[kMaxSlots];
+    __shared__ __attribute__((aligned(16))) float z[kShares][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15, n0 = blockIdx.x * 16;
+    for (int s = threadIdx.x; s < p.slots; s += NT) {
+        expert[s] = p.plan->expert[s];
+        start[s] = p.plan->start[s];
+        place[s] = p.plan->row[s];
+    }
+    const int active = __builtin_amdgcn_readfirstlane(p.plan->active), held = __builtin_amdgcn_readfirstlane(p.plan->held);
+    __syncthreads();
+    const int count = (p.inner + Q::SUB * kStep - 1) / (Q::SUB * kStep);
+    // shares of K: as many as make the waves' iterations fewest, two lost to each task's start
+    int shares = 1, least = INT32_MAX;
+    for (int s = 1; s <= W && s <= count && s * held <= kShares; s *= 2) {
+        const int cost = (active * s + W - 1) / W * ((count + s - 1) / s + 2);
+        if (cost < least) { least = cost; shares = s; }
+    }
+    const int shift = __builtin_ctz(shares);
+    for (int task = wave; task < active * shares; task += W) {
+        const int index = task >> shift, share = task & (shares - 1);
+        const int e = __builtin_amdgcn_readfirstlane(expert[index]), base = __builtin_amdgcn_readfirstlane(start[index]),
+                  rows = (index + 1 < active ? __builtin_amdgcn_readfirstlane(start[index + 1]) : held) - base;
+        Q w[1];
+        w[0].at(p.wout, p.ld_out, p.sout, p.ld_sout, (long)e * p.width + min(n0 + r, p.width - 1), p.inner);
+        for (int t0 = 0; t0 < rows; t0 += PER) {
+            const int at = t0 + r / PH;
+            Activations<__bf16, Q::SUB> x;
+            x.row = p.h + ((long)(base + min(at, rows - 1)) * PH + r % PH) * p.ld_h;
+            x.part = 0;
+            x.k = p.inner;
+            f32x4 acc[1] = {};
+            multiply<RAGGED, Q, __bf16, 1>(w, x, share, shares, g, acc);
+            f32x4 v;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                float sum = acc[0][c];
+#pragma unroll
+                for (int o = 1; o < PH; ++o) sum += __shfl_down(acc[0][c], o);
+                v[c] = sum;
+            }
+            if (r < PER * PH && r % PH == 0 && at < rows) *(f32x4 *)&z[share * held + base + at][g * 4] = v;
+        }
+    }
+    __syncthreads();
+    for (int o = threadIdx.x; o < p.tokens * 16; o += NT) {
+        const int t = o / 16, c = o % 16;
+        if (n0 + c >= p.width) continue;
+        float y = 0.f;
+        for (int j = 0; j < p.k; ++j) {
+            const int s = t * p.k + j, row = place[s];
+            if (row < 0) continue;
+            float sum = 0.f;
+            for (int u = 0; u < shares; ++u) sum += z[u * held + row][c];
+            sum *= Q::scale(p.sout, (long)p.expert[s] * p.width + n0 + c);
+            y = fmaf(p.weight ? p.weight[s] : 1.f, sum, y);
+        }
+        ((T *)p.y)[t * p.ld_y + n0 + c] = narrow<T>(y);
+    }
+}
+
+// ------------------------------------------------------------------ host side
+using opevo::launch;
+
+int check_layer(const char *who, int64_t tokens, int k, int experts, int dtype, int64_t width, int64_t inner)
+{
+    if (!known(dtype)) return fail(OPEVO_E_ARG, "%s: unknown element type %d", who, dtype);
+    if (tokens < 0 || k < 1 || k > OPEVO_ROUTE_MAX_SLOTS || tokens > kMaxSlots / k)
+        return fail(OPEVO_E_ARG, "%s: tokens %lld with %d slots each (1 to %d, %d in all)", who, (long long)tokens, k, OPEVO_ROUTE_MAX_SLOTS, kMaxSlots);
+    if (experts < 1 || experts > OPEVO_ROUTE_MAX_EXPERTS) return fail(OPEVO_E_ARG, "%s: %d experts (1 to %d)", who, experts, OPEVO_ROUTE_MAX_EXPERTS);
+    constexpr int64_t most = 1 << 20;
+    if (width < 1 || width > most || inner < 1 || inner > most)
+        return fail(OPEVO_E_ARG, "%s: %lld channels and %lld inner ones (1 to 2^20)", who, (long long)width, (long long)inner);
+    return OPEVO_OK;
+}
+
+int64_t row_of_h(int64_t inner) { return (inner + 7) / 8 * 8; }
+size_t layer_workspace(int64_t slots, int dtype, int64_t inner) { return sizeof(Plan) + (size_t)slots * (dtype == OPEVO_F32 ? 3 : 2) * row_of_h(inner) * sizeof(__bf16); }
+
+template <typename T, typename Q>
+int run_layer(const Layer &p, hipStream_t stream)
+{
+    const int groups = std::min(p.slots, p.experts);
+    constexpr int LONG = Q::SUB * kStep;
+    const bool ragged_in = p.width % LONG != 0, ragged_out = p.inner % LONG != 0;
+    const int per = ragged_in ? 16 : 32;
+    if (int rc = launch("layer_in launch", ragged_in ? layer_in<T, Q, 4, true> : layer_in<T, Q, 4, false>, dim3((p.inner + per - 1) / per, groups + 1), dim3(256), stream, p)) return rc;
+    return launch("layer_out launch", ragged_out ? layer_out<T, Q, 8, true> : layer_out<T, Q, 8, false>, dim3((p.width + 15) / 16), dim3(512), stream, p);
+}
+template <typename T> int run_layer8(const Layer &p, hipStream_t stream) { return run_layer<T, Weights8>(p, stream); }
+template <typename T> int run_layer4(const Layer &p, hipStream_t stream) { return run_layer<T, Weights4>(p, stream); }
+
+// The checks that both kinds of weights share, and where things stand in the workspace.
+int plan_layer(const char *who, Layer *p, int dtype, int64_t tokens, int k, int experts, int64_t width, int64_t inner, void *workspace, size_t bytes)
+{
+    const size_t size = size_of(dtype);
+    if (int rc = check_rows(who, "x", p->x, p->ld_x, width, size)) return rc;
+    if (int rc = check_rows(who, "y", p->y, p->ld_y, width, size)) return rc;
+    if (int rc = check_words(who, "expert", p->expert)) return rc;
+    if (!aligned(p->weight, 4)) return fail(OPEVO_E_ARG, "%s: weight is not aligned to 4 bytes", who);
+    const size_t need = layer_workspace(tokens * k, dtype, inner);
+    if (!workspace || !aligned(workspace, 16) || bytes < need)
+        return fail(OPEVO_E_ARG, "%s: the workspace holds %zu bytes of the %zu it takes, or is not aligned to 16 bytes", who, workspace ? bytes : 0, need);
+    p->tokens = (int)tokens; p->k = k; p->slots = (int)tokens * k; p->experts = experts; p->width = (int)width; p->inner = (int)inner;
+    p->plan = static_cast<Plan *>(workspace);
+    p->h = reinterpret_cast<__bf16 *>(p->plan + 1);
+    p->ld_h = row_of_h(inner);
+    return OPEVO_OK;
+}
+
+}  // namespace
+
+extern "C" int opevo_expert_layer_workspace(int64_t tokens, int k, int dtype, int64_t inner, size_t *bytes)
+{
+    const char *who = "expert_layer_workspace";
+    if (!bytes) return fail(OPEVO_E_ARG, "%s: bytes is NULL", who);
+    if (int rc = check_layer(who, tokens, k, 1, dtype, 1, inner)) return rc;
+    *bytes = tokens == 0 ? 0 : layer_workspace(tokens * k, dtype, inner);
+    return OPEVO_OK;
+}
+
+extern "C" int opevo_expert_layer_i8(const void *x, int64_t ld_x, int dtype, const int32_t *expert, const float *weight, int64_t tokens, int k, int experts, int64_t width,
+                                     int64_t inner, const int8_t *w_in, int64_t ld_in, const float *scale_in, const int8_t *w_out, int64_t ld_out, const float *scale_out,
+                                     void *y, int64_t ld_y, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *who = "expert_layer_i8";
+    if (int rc = check_layer(who, tokens, k, experts, dtype, width, inner)) return rc;
+    if (tokens == 0) return OPEVO_OK;
+    Layer p = {};
+    p.x = x; p.ld_x = (long)ld_x; p.expert = expert; p.weight = weight; p.y = y; p.ld_y = (long)ld_y;
+    p.win = reinterpret_cast<const uint8_t *>(w_in); p.ld_in = (long)ld_in; p.sin = scale_in;
+    p.wout = reinterpret_cast<const uint8_t *>(w_out); p.ld_out = (long)ld_out; p.sout = scale_out;
+    if (int rc = check_rows(who, "w_in", w_in, ld_in, width, 1)) return rc;
+    if (int rc = check_words(who, "scale_in", scale_in)) return rc;
+    if (int rc = check_rows(who, "w_out", w_out, ld_out, inner, 1)) return rc;
+    if (int rc = check_words(who, "scale_out", scale_out)) return rc;
+    if (int rc = plan_layer(who, &p, dtype, tokens, k, experts, width, inner, workspace, workspace_bytes)) return rc;
+    return BY_DTYPE(dtype, run_layer8, p, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int opevo_expert_layer_mx4(const void *x, int64_t ld_x, int dtype, const int32_t *expert, const float *weight, int64_t tokens, int k, int experts, int64_t width,
+                                      int64_t inner, const uint8_t *w_in, int64_t ld_in, const uint8_t *scale_in, int64_t ld_scale_in, const uint8_t *w_out, int64_t ld_out,
+                                      const uint8_t *scale_out, int64_t ld_scale_out, void *y, int64_t ld_y, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *who = "expert_layer_mx4";
+    if (int rc = check_layer(who, tokens, k, experts, dtype, width, inner)) return rc;
+    if (tokens == 0) return OPEVO_OK;
+    Layer p = {};
+    p.x = x; p.ld_x = (long)ld_x; p.expert = expert; p.weight = weight; p.y = y; p.ld_y = (long)ld_y;
+    p.win = w_in; p.ld_in = (long)ld_in; p.sin = scale_in; p.ld_sin = (long)ld_scale_in;
+    p.wout = w_out; p.ld_out = (long)ld_out; p.sout = scale_out; p.ld_sout = (long)ld_scale_out;
+    if (int rc = check_rows(who, "w_in", w_in, ld_in, (width + 1) / 2, 1)) return rc;
+    if (int rc = check_rows(who, "scale_in", scale_in, ld_scale_in, (width + 31) / 32, 1)) return rc;
+    if (int rc = check_rows(who, "w_out", w_out, ld_out, (inner + 1) / 2, 1)) return rc;
+    if (int rc = check_rows(who, "scale_out", scale_out, ld_scale_out, (inner + 31) / 32, 1)) return rc;
+    if (int rc = plan_layer(who, &p, dtype, tokens, k, experts, width, inner, workspace, workspace_bytes)) return rc;
+    return BY_DTYPE(dtype, run_layer4, p, static_cast<hipStream_t>(stream));
+}

@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "launch.hpp"
+#include "mx4.hpp"
 #include "narrow.hpp"
 #include "product.hpp"
 #include "rows.hpp"
@@ -62,27 +63,6 @@ __device__ __forceinline__ f32x4 mfma_at(int at_b, int at_a, i32x4 b, i32x4 a, f
     case 14: return mfma<3, 2>(b, a, c, sb, sa);
     default: return mfma<3, 3>(b, a, c, sb, sa);
     }
-}
-
-// 16 bytes of a row from byte k on, zeros past its end (and in the half byte past an odd K).
-__device__ __forceinline__ i32x4 load_codes(const uint8_t *row, int k, int end, bool odd)
-{
-    i32x4 v = load_chunk((const int8_t *)row, k, end);
-    const int last = end - 1 - k;
-    if (odd && last >= 0 && last < 16)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (last >> 2 == i) v[i] &= ~(0xf0 << 8 * (last & 3));
-    return v;
-}
-// Four factors of a row from block b on, zeros past its end: with codes of zero any factor but NaN gives zero.
-__device__ __forceinline__ int load_factors(const uint8_t *row, int b, int blocks)
-{
-    int v = 0;
-    if (b + 4 <= blocks) __builtin_memcpy(&v, row + b, 4);
-    else
-        for (int i = 0; b + i < blocks; ++i) v |= (int)row[b + i] << 8 * i;
-    return v;
 }
 
 // Writes a wave's MI x NI atoms, rows r.first + m0 .. and columns col0 .. of C.  Lane l of an atom holds columns 4 * (l / 16) .. + 3 of row l % 16; the 16 rows of an atom row go through a

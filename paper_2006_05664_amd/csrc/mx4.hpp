@@ -4,11 +4,35 @@
 
 #include <hip/hip_runtime.h>
 
+#include "product.hpp"
+
 namespace {
 
 constexpr int kMx4NaN = 255;
 
 // The factor in fp32.  2^-127 is subnormal there; the conversions take it.
 __device__ __forceinline__ float mx4_factor(int b) { return __uint_as_float(b == kMx4NaN ? 0x7fc00000u : b == 0 ? 0x00400000u : (unsigned)b << 23); }
+
+// Codes from byte k of a row on that ends at byte `end`, the last one of which has half a byte too many where `odd`.
+__device__ __forceinline__ i32x4 without_half_byte(i32x4 v, int k, int end, bool odd)
+{
+    const int last = end - 1 - k;
+    if (odd && last >= 0 && last < 16)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (last >> 2 == i) v[i] &= ~(0xf0 << 8 * (last & 3));
+    return v;
+}
+// 16 bytes of a row from byte k on, zeros past its end (and in the half byte past an odd K).
+__device__ __forceinline__ i32x4 load_codes(const uint8_t *row, int k, int end, bool odd) { return without_half_byte(load_chunk((const int8_t *)row, k, end), k, end, odd); }
+// Four factors of a row from block b on, zeros past its end: with codes of zero any factor but NaN gives zero.
+__device__ __forceinline__ int load_factors(const uint8_t *row, int b, int blocks)
+{
+    int v = 0;
+    if (b + 4 <= blocks) __builtin_memcpy(&v, row + b, 4);
+    else
+        for (int i = 0; b + i < blocks; ++i) v |= (int)row[b + i] << 8 * i;
+    return v;
+}
 
 }  // namespace
