@@ -14,18 +14,24 @@
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;           // of a workgroup; as many as a row's lanes where those are more
+constexpr int kMostLanes = 512;
 
-// A row's pieces of 16 bytes.  The last one may be short and is then taken element by element: no element belongs to two pieces, so a lane may write where it has read
-// (a sum in place of the residual) whatever other lanes have still to read.
-template <typename T> struct Row {
+// How a row falls into pieces of 16 bytes.  kWhole: without a rest.  kOverlap: the last piece ends with the row and shares elements with the one before it; both write the same values, after
+// all pieces of the row have been read (a sum may stand in the place of an input), so the row has to be held in registers.  kRest: the last piece is taken element by element, which
+// makes branches of every access (32 rows of 4096 bf16: 4.2 us instead of 3.4).
+enum Way { kWhole, kOverlap, kRest };
+template <typename T, Way WAY> struct Row {
     static constexpr int n = Vec<T>::n;
     int width, count;
     __device__ explicit Row(int w) : width(w), count((w + n - 1) / n) {}
+    __device__ __forceinline__ int first(int i) const { return WAY == kOverlap ? min(i * n, width - n) : i * n; }
+    // how many of its elements the piece before has too
+    __device__ __forceinline__ int twice(int i) const { return WAY == kOverlap ? i * n - first(i) : 0; }
     __device__ __forceinline__ Vec<T> load(const T *row, int i) const
     {
         Vec<T> v = {};
-        if (i * n + n <= width) __builtin_memcpy(&v, row + i * n, 16);
+        if (WAY != kRest || i * n + n <= width) __builtin_memcpy(&v, row + first(i), 16);
         else
 #pragma unroll
             for (int e = 0; e < n; ++e)
@@ -34,7 +40,7 @@ template <typename T> struct Row {
     }
     template <typename O> __device__ __forceinline__ void store(O *row, int i, const O (&v)[n]) const
     {
-        if (i * n + n <= width) __builtin_memcpy(row + i * n, v, sizeof v);
+        if (WAY != kRest || i * n + n <= width) __builtin_memcpy(row + first(i), v, sizeof v);
         else
 #pragma unroll
             for (int e = 0; e < n; ++e)
@@ -43,17 +49,16 @@ template <typename T> struct Row {
 };
 
 // Lanes of a row: `tx` side by side, a power of two.  What they hold is combined in an order that depends on tx alone.
-template <typename V, typename F>
-__device__ __forceinline__ V of_row(V v, int tx, V (&red)[kThreads / 64], F &&f)
+template <typename V, typename F> __device__ __forceinline__ V of_wave(V v, int tx, F &&f)
 {
     for (int o = 1; o < tx && o < 64; o <<= 1) v = f(v, (V)__shfl_xor(v, o));
-    if (tx > 64) {                          // alike for the whole workgroup
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-        __syncthreads();
-        const int w0 = (int)((threadIdx.x >> __builtin_ctz(tx)) << (__builtin_ctz(tx) - 6));
-        v = red[w0];
-        for (int w = 1; w < tx / 64; ++w) v = f(v, red[w0 + w]);
-    }
+    return v;
+}
+template <typename V, typename F> __device__ __forceinline__ V of_waves(const V *red, int tx, F &&f)
+{
+    const int w0 = (int)((threadIdx.x >> __builtin_ctz(tx)) << (__builtin_ctz(tx) - 6));
+    V v = red[w0];
+    for (int w = 1; w < tx / 64; ++w) v = f(v, red[w0 + w]);
     return v;
 }
 
@@ -62,7 +67,7 @@ template <typename T> struct Exact { typedef float type; };
 template <> struct Exact<float> { typedef double type; };
 
 // q = round(127 v / a).  v times 127 / a in fp32 is off by at most three roundings, 127 * 3 * 2^-24 = 2.3e-5, and rounds to the same integer unless it is within 4e-5 of
-// the middle between two; then the quotient is formed in fp64, where the middle is hit only by quotients that are there.
+// the middle between two; then the quotients of the piece are formed in fp64, where the middle is hit only by quotients that are there.
 template <typename V> struct RowTo8 {
     V a;
     float inv, pre;
@@ -73,13 +78,19 @@ template <typename V> struct RowTo8 {
         inv = 127.f / (float)(a * (V)pre);
         on = a > 0 && a <= (V)FLT_MAX;
     }
-    __device__ __forceinline__ int8_t operator()(V v) const
+    template <int N> __device__ __forceinline__ void operator()(const V (&v)[N], int8_t (&q)[N]) const
     {
         constexpr float kRound = 12582912.f;                // 1.5 * 2^23: what is added to it is rounded to an integer, in its low bits
-        const float f = (float)(v * (V)pre), r = fmaf(f, inv, kRound);
-        int q = (int)(__float_as_uint(r) & 0xff);
-        if (fabsf(fmaf(f, inv, kRound - r)) > 0.49996f) q = (int)rint(127.0 * (double)v / (double)a);
-        return (int8_t)(on ? q : 0);
+        float off = 0.f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float f = (float)(v[e] * (V)pre), r = fmaf(f, inv, kRound);
+            off = fmaxf(off, fabsf(fmaf(f, inv, kRound - r)));
+            q[e] = (int8_t)(on ? (int)(__float_as_uint(r) & 0xff) : 0);
+        }
+        if (on && off > 0.49996f)
+#pragma unroll 1
+            for (int e = 0; e < N; ++e) q[e] = (int8_t)(int)rint(127.0 * (double)v[e] / (double)a);
     }
 };
 
@@ -96,26 +107,26 @@ struct Norm {
     float eps;
 };
 
-template <typename T, int HOLD, bool TO8>
-__global__ __launch_bounds__(kThreads)
+// 16384 rows of 4096 bf16 with a residual: 537 MB in 90 - 94 us (5.8 TB/s; a large copy takes 104 for as many bytes); in 8 bits 84.  32 rows: 3.2 us, a launch and a
+// chain of latencies.  As many lanes as a row has pieces, up to 512: with two pieces on 256 lanes it takes 94 us, with four on 128 as much, with eight on 64 147.
+template <typename T, int HOLD, bool TO8, Way WAY>
+__global__ __launch_bounds__(kMostLanes)
 void norm_rows(Norm p)
 {
     typedef typename Exact<T>::type V;
     constexpr int n = Vec<T>::n;
-    __shared__ float red[kThreads / 64];
-    __shared__ V red8[kThreads / 64];
-    const int tx = p.tx, lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx);
-    const long row = this_block() * ty + ((int)threadIdx.x >> __builtin_ctz(tx));
+    __shared__ float red[kMostLanes / 64];
+    __shared__ V red8[kMostLanes / 64];
+    const int tx = p.tx, lane = (int)threadIdx.x & (tx - 1);
+    const long row = this_block() * (blockDim.x >> __builtin_ctz(tx)) + (threadIdx.x >> __builtin_ctz(tx));
     const bool on = row < p.rows;
-    const Row<T> at(on ? p.width : 0);
+    const Row<T, WAY> at(p.width);
+    const int count = on ? at.count : 0;
     const T *x = (const T *)p.x + row * p.ld_x, *r = (const T *)p.residual + row * p.ld_residual, *w = (const T *)p.weight;
-    auto summed = [&](int i) {
-        Vec<T> s = at.load(x, i);
-        if (p.residual) {
-            const Vec<T> add = at.load(r, i);
+    auto summed = [&](const Vec<T> &x, const Vec<T> &r) {
+        Vec<T> s;
 #pragma unroll
-            for (int e = 0; e < n; ++e) s.v[e] = narrow<T>((float)s.v[e] + (float)add.v[e]);
-        }
+        for (int e = 0; e < n; ++e) s.v[e] = narrow<T>((float)x.v[e] + (float)r.v[e]);
         return s;
     };
     auto weights = [&](int i) {
@@ -125,30 +136,33 @@ void norm_rows(Norm p)
         for (int e = 0; e < n; ++e) one.v[e] = (T)1.f;
         return one;
     };
-    Vec<T> s[HOLD], add[HOLD];
+    Vec<T> s[HOLD], by[HOLD];
 #pragma unroll
-    for (int u = 0; u < HOLD; ++u) {
-        s[u] = {};
-        if (lane + u * tx < at.count) s[u] = at.load(x, lane + u * tx);
-    }
+    for (int u = 0; u < HOLD; ++u)
+        if (lane + u * tx < count) s[u] = at.load(x, lane + u * tx);
     if (p.residual) {
-#pragma unroll
-        for (int u = 0; u < HOLD; ++u) {
-            add[u] = {};
-            if (lane + u * tx < at.count) add[u] = at.load(r, lane + u * tx);
-        }
+        Vec<T> add[HOLD];
 #pragma unroll
         for (int u = 0; u < HOLD; ++u)
+            if (lane + u * tx < count) add[u] = at.load(r, lane + u * tx);
 #pragma unroll
-            for (int e = 0; e < n; ++e) s[u].v[e] = narrow<T>((float)s[u].v[e] + (float)add[u].v[e]);
+        for (int u = 0; u < HOLD; ++u)
+            if (lane + u * tx < count) by[u] = weights(lane + u * tx);
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u)
+            if (lane + u * tx < count) s[u] = summed(s[u], add[u]);
+    } else {
+#pragma unroll
+        for (int u = 0; u < HOLD; ++u)
+            if (lane + u * tx < count) by[u] = weights(lane + u * tx);
     }
     float squares = 0.f;
     V most = 0;
-    auto look = [&](int i, const Vec<T> &v) {
+    auto look = [&](int twice, const Vec<T> &v, const Vec<T> &by) {
 #pragma unroll
-        for (int e = 0; e < n; ++e) squares = fmaf((float)v.v[e], (float)v.v[e], squares);
+        for (int e = 0; e < n; ++e)
+            if (e >= twice) squares = fmaf((float)v.v[e], (float)v.v[e], squares);
         if (TO8) {
-            const Vec<T> by = weights(i);
 #pragma unroll
             for (int e = 0; e < n; ++e) {
                 V m = fabs((V)v.v[e] * (V)by.v[e]);
@@ -159,21 +173,36 @@ void norm_rows(Norm p)
     };
 #pragma unroll
     for (int u = 0; u < HOLD; ++u)
-        if (lane + u * tx < at.count) look(lane + u * tx, s[u]);
-    for (int i = lane + HOLD * tx; i < at.count; i += tx) look(i, summed(i));
-    squares = of_row(squares, tx, red, [](float a, float b) { return a + b; });
+        if (lane + u * tx < count) look(at.twice(lane + u * tx), s[u], by[u]);
+    // pieces that no lane holds are read, and added up, once more when they are written
+    auto again = [&](int i) { return p.residual ? summed(at.load(x, i), at.load(r, i)) : at.load(x, i); };
+    if (WAY != kOverlap)
+        for (int i = lane + HOLD * tx; i < count; i += tx) look(0, again(i), weights(i));
+    const auto add = [](float a, float b) { return a + b; };
+    const auto larger = [](V a, V b) { return fmax(a, b); };
+    squares = of_wave(squares, tx, add);
+    if (TO8) most = of_wave(most, tx, larger);
+    if (tx > 64) {                          // alike for the whole workgroup
+        if ((threadIdx.x & 63) == 0) {
+            red[threadIdx.x >> 6] = squares;
+            if (TO8) red8[threadIdx.x >> 6] = most;
+        }
+        __syncthreads();
+        squares = of_waves(red, tx, add);
+        if (TO8) most = of_waves(red8, tx, larger);
+    }
     const float inv = 1.f / sqrtf(squares / (float)p.width + p.eps);
-    if (TO8) most = of_row(most, tx, red8, [](V a, V b) { return fmax(a, b); });
     if (!on) return;
     const RowTo8<V> to8(most);
     T *sum = (T *)p.sum + row * p.ld_sum;
-    auto write = [&](int i, const Vec<T> &v) {
+    auto write = [&](int i, const Vec<T> &v, const Vec<T> &by) {
         if (p.sum) at.store(sum, i, v.v);
-        const Vec<T> by = weights(i);
         if constexpr (TO8) {
+            V product[n];
             int8_t q[n];
 #pragma unroll
-            for (int e = 0; e < n; ++e) q[e] = to8((V)v.v[e] * (V)by.v[e]);
+            for (int e = 0; e < n; ++e) product[e] = (V)v.v[e] * (V)by.v[e];
+            to8(product, q);
             at.store((int8_t *)p.y + row * p.ld_y, i, q);
         } else {
             Vec<T> y;
@@ -184,8 +213,9 @@ void norm_rows(Norm p)
     };
 #pragma unroll
     for (int u = 0; u < HOLD; ++u)
-        if (lane + u * tx < at.count) write(lane + u * tx, s[u]);
-    for (int i = lane + HOLD * tx; i < at.count; i += tx) write(i, summed(i));
+        if (lane + u * tx < count) write(lane + u * tx, s[u], by[u]);
+    if (WAY != kOverlap)
+        for (int i = lane + HOLD * tx; i < count; i += tx) write(i, again(i), weights(i));
     if (lane == 0 && p.per_row) p.per_row[row] = !TO8 ? inv : most <= (V)FLT_MAX ? (float)(most * (V)inv / (V)127) : __uint_as_float(0x7fc00000u);
 }
 
@@ -201,15 +231,17 @@ struct Grad {
     int width, tx;
 };
 
-template <typename T, int HOLD>
-__global__ __launch_bounds__(kThreads)
+// Bound by memory: 8192 rows of 4096 bf16 with a gradient of the sum, 268 MB, in 47 us (5.7 TB/s) and 2.9 for the weight's partial sums.  A workgroup goes from row to row, the next one on its way,
+// with its share of the weight's gradient in registers; 512 workgroups (256: 66 us, 1024: 52).
+template <typename T, int HOLD, Way WAY>
+__global__ __launch_bounds__(kMostLanes)
 void norm_grad(Grad p)
 {
     constexpr int n = Vec<T>::n;
-    __shared__ float red[2][kThreads / 64];
-    __shared__ float part[HOLD * kThreads * n];
-    const int tx = p.tx, lane = (int)threadIdx.x & (tx - 1), ty = kThreads >> __builtin_ctz(tx), line = (int)threadIdx.x >> __builtin_ctz(tx);
-    const Row<T> at(p.width);
+    __shared__ float red[2][kMostLanes / 64];
+    __shared__ float part[HOLD * kMostLanes * n];
+    const int tx = p.tx, lane = (int)threadIdx.x & (tx - 1), ty = (int)blockDim.x >> __builtin_ctz(tx), line = (int)threadIdx.x >> __builtin_ctz(tx);
+    const Row<T, WAY> at(p.width);
     const T *w = (const T *)p.weight;
     auto weights = [&](int i) {
         if (w) return at.load(w, i);
@@ -227,45 +259,49 @@ void norm_grad(Grad p)
     }
     float *own = p.dw ? p.dw + (long)blockIdx.x * p.width : nullptr;
     const long step = (long)gridDim.x * ty;
-    Vec<T> g[HOLD], s[HOLD], next_g[HOLD], next_s[HOLD];
-    auto load = [&](Vec<T> (&g)[HOLD], Vec<T> (&s)[HOLD], long row) {
+    struct Pieces { Vec<T> g[HOLD], s[HOLD], add[HOLD]; float inv; } a, b;
+    auto load = [&](Pieces &to, long row) {
+        const bool on = row < p.rows;
+        to.inv = on ? p.inv_rms[row] : 0.f;
 #pragma unroll
         for (int u = 0; u < HOLD; ++u) {
-            g[u] = {};
-            s[u] = {};
-            if (row < p.rows && lane + u * tx < at.count) {
-                g[u] = at.load((const T *)p.dy + row * p.ld_dy, lane + u * tx);
-                s[u] = at.load((const T *)p.sum + row * p.ld_sum, lane + u * tx);
+            const int i = lane + u * tx;
+            to.g[u] = to.s[u] = to.add[u] = {};
+            if (on && i < at.count) {
+                to.g[u] = at.load((const T *)p.dy + row * p.ld_dy, i);
+                to.s[u] = at.load((const T *)p.sum + row * p.ld_sum, i);
+                if (p.dsum) to.add[u] = at.load((const T *)p.dsum + row * p.ld_dsum, i);
             }
         }
     };
-    int turn = 0;
-    long row = (long)blockIdx.x * ty + line;
-    load(g, s, row);
-    // rows of a workgroup's lines in step: of_row meets all its threads
-    for (long row0 = (long)blockIdx.x * ty; row0 < p.rows; row0 += step, row += step, turn ^= 1) {
+    // A row of this line, the next one on its way.  All lines of a workgroup go in step: their sums meet.
+    auto step_of = [&](const Pieces &now, Pieces &next, long row, int turn) {
         const bool on = row < p.rows;
-        const T *dy = (const T *)p.dy + row * p.ld_dy, *sum = (const T *)p.sum + row * p.ld_sum;
-        load(next_g, next_s, row + step);
-        const float inv = on ? p.inv_rms[row] : 0.f;
-        Vec<T> add[HOLD];
-#pragma unroll
-        for (int u = 0; u < HOLD; ++u) {
-            add[u] = {};
-            if (p.dsum && on && lane + u * tx < at.count) add[u] = at.load((const T *)p.dsum + row * p.ld_dsum, lane + u * tx);
-        }
+        load(next, row + step);
         float dot = 0.f;
 #pragma unroll
-        for (int u = 0; u < HOLD; ++u)
+        for (int u = 0; u < HOLD; ++u) {
+            const int twice = at.twice(lane + u * tx);
 #pragma unroll
-            for (int e = 0; e < n; ++e) dot = fmaf((float)by[u].v[e] * (float)g[u].v[e], (float)s[u].v[e], dot);
-        for (int i = lane + HOLD * tx; on && i < at.count; i += tx) {
-            const Vec<T> gi = at.load(dy, i), si = at.load(sum, i), wi = weights(i);
-#pragma unroll
-            for (int e = 0; e < n; ++e) dot = fmaf((float)wi.v[e] * (float)gi.v[e], (float)si.v[e], dot);
+            for (int e = 0; e < n; ++e)
+                if (e >= twice) dot = fmaf((float)by[u].v[e] * (float)now.g[u].v[e], (float)now.s[u].v[e], dot);
         }
-        dot = of_row(dot, tx, red[turn], [](float a, float b) { return a + b; });
-        const float back = inv * inv * (dot / (float)p.width);
+        const T *dy = (const T *)p.dy + row * p.ld_dy, *sum = (const T *)p.sum + row * p.ld_sum;
+        if (WAY != kOverlap)
+            for (int i = lane + HOLD * tx; on && i < at.count; i += tx) {
+                const Vec<T> gi = at.load(dy, i), si = at.load(sum, i), wi = weights(i);
+#pragma unroll
+                for (int e = 0; e < n; ++e) dot = fmaf((float)wi.v[e] * (float)gi.v[e], (float)si.v[e], dot);
+            }
+        const auto plus = [](float a, float b) { return a + b; };
+        dot = of_wave(dot, tx, plus);
+        if (tx > 64) {
+            if ((threadIdx.x & 63) == 0) red[turn][threadIdx.x >> 6] = dot;
+            __syncthreads();
+            dot = of_waves(red[turn], tx, plus);
+        }
+        if (!on) return;
+        const float inv = now.inv, back = inv * inv * (dot / (float)p.width);
         auto write = [&](int i, const Vec<T> &gi, const Vec<T> &si, const Vec<T> &wi, const Vec<T> &ai) {
             Vec<T> out;
 #pragma unroll
@@ -275,14 +311,14 @@ void norm_grad(Grad p)
             }
             at.store((T *)p.dx + row * p.ld_dx, i, out.v);
         };
-        if (on) {
 #pragma unroll
-            for (int u = 0; u < HOLD; ++u) {
-                if (lane + u * tx < at.count) write(lane + u * tx, g[u], s[u], by[u], add[u]);
+        for (int u = 0; u < HOLD; ++u) {
+            if (lane + u * tx < at.count) write(lane + u * tx, now.g[u], now.s[u], by[u], now.add[u]);
 #pragma unroll
-                for (int e = 0; e < n; ++e) dw[u][e] = fmaf((float)g[u].v[e], (float)s[u].v[e] * inv, dw[u][e]);
-            }
-            // pieces that no lane holds: tx is the whole workgroup then (ty = 1), and their partial sums stay in memory, each a lane's own
+            for (int e = 0; e < n; ++e) dw[u][e] = fmaf((float)now.g[u].v[e], (float)now.s[u].v[e] * inv, dw[u][e]);
+        }
+        // pieces that no lane holds: a row has the whole workgroup then, and their partial sums stay in memory, each a lane's own
+        if (WAY != kOverlap)
             for (int i = lane + HOLD * tx; i < at.count; i += tx) {
                 const Vec<T> gi = at.load(dy, i), si = at.load(sum, i), wi = weights(i);
                 Vec<T> ai = {};
@@ -290,12 +326,15 @@ void norm_grad(Grad p)
                 if (own)
 #pragma unroll
                     for (int e = 0; e < n; ++e)
-                        if (i * n + e < p.width) own[i * n + e] = fmaf((float)gi.v[e], (float)si.v[e] * inv, row0 == (long)blockIdx.x ? 0.f : own[i * n + e]);
+                        if (i * n + e < p.width) own[i * n + e] = fmaf((float)gi.v[e], (float)si.v[e] * inv, row == (long)blockIdx.x ? 0.f : own[i * n + e]);
                 write(i, gi, si, wi, ai);
             }
-        }
-#pragma unroll
-        for (int u = 0; u < HOLD; ++u) { g[u] = next_g[u]; s[u] = next_s[u]; }
+    };
+    long row = (long)blockIdx.x * ty + line;
+    load(a, row);
+    for (long row0 = (long)blockIdx.x * ty; row0 < p.rows; row0 += 2 * step, row += 2 * step) {
+        step_of(a, b, row, 0);
+        if (row0 + step < p.rows) step_of(b, a, row + step, 1);
     }
     if (!own) return;
     // the lines' sums, one line after the other
@@ -311,12 +350,12 @@ void norm_grad(Grad p)
         __syncthreads();
     }
     const int held = min(p.width, HOLD * tx * n);
-    for (int c = threadIdx.x; c < held; c += kThreads) {
+    for (int c = threadIdx.x; c < held; c += blockDim.x) {
         const int i = c / n, u = i / tx;
-        own[c] = part[(c % n * HOLD + u) * tx + i - u * tx];
+        own[c] = part[((c - at.first(i)) * HOLD + u) * tx + i - u * tx];
     }
     if (p.rows == 0)
-        for (int c = held + threadIdx.x; c < p.width; c += kThreads) own[c] = 0.f;
+        for (int c = held + threadIdx.x; c < p.width; c += blockDim.x) own[c] = 0.f;
 }
 
 // dw[c] = the sum of part[0 .. parts][c]: kCols columns a workgroup, a part of the lines each thread, joined in the LDS.
@@ -343,14 +382,13 @@ void norm_grad_weight(const float *__restrict__ part, int parts, int width, floa
 // ------------------------------------------------------------------ host side
 using opevo::launch;
 
-// `tx` lanes to a row of `pieces`, `hold` pieces a lane.
+// `tx` lanes to a row of `pieces`, at most `lanes` of them, `hold` pieces a lane.
 struct Shape { int tx, hold; };
-Shape shape_of(int64_t pieces, int64_t rows, int most)
+Shape shape_of(int64_t pieces, int lanes, int most)
 {
     int tx = 1, hold = 1;
-    while (tx < kThreads && tx < pieces) tx *= 2;
+    while (tx < lanes && tx < pieces) tx *= 2;
     while (hold < most && (int64_t)tx * hold < pieces) hold *= 2;
-    while (tx > 64 && hold < most && rows * (tx / 2) / 64 >= 4096) { tx /= 2; hold *= 2; }
     return {tx, hold};
 }
 
@@ -374,11 +412,16 @@ int check_norm(const char *who, const Norm &p, int dtype, int64_t rows, int64_t 
 template <typename T, bool TO8>
 int run_norm(Norm p, hipStream_t stream)
 {
-    const Shape l = shape_of((p.width + Vec<T>::n - 1) / Vec<T>::n, p.rows, 8);
+    constexpr int n = Vec<T>::n;
+    const int64_t pieces = (p.width + n - 1) / n;
+    const Shape l = shape_of(pieces, kMostLanes, 4);
+    const bool held = pieces <= (int64_t)l.tx * l.hold;
     p.tx = l.tx;
-    const int ty = kThreads / l.tx;
-    auto *k = l.hold == 1 ? norm_rows<T, 1, TO8> : l.hold == 2 ? norm_rows<T, 2, TO8> : l.hold == 4 ? norm_rows<T, 4, TO8> : norm_rows<T, 8, TO8>;
-    return launch("norm_rows launch", k, spread((p.rows + ty - 1) / ty), dim3(kThreads), stream, p);
+    const int threads = std::max(l.tx, kThreads), ty = threads / l.tx;
+    auto *k = p.width % n == 0 ? (l.hold == 1 ? norm_rows<T, 1, TO8, kWhole> : l.hold == 2 ? norm_rows<T, 2, TO8, kWhole> : norm_rows<T, 4, TO8, kWhole>)
+              : p.width > n && held ? (l.hold == 1 ? norm_rows<T, 1, TO8, kOverlap> : l.hold == 2 ? norm_rows<T, 2, TO8, kOverlap> : norm_rows<T, 4, TO8, kOverlap>)
+                                    : norm_rows<T, 1, TO8, kRest>;
+    return launch("norm_rows launch", k, spread((p.rows + ty - 1) / ty), dim3(threads), stream, p);
 }
 template <typename T> int run_plain(const Norm &p, hipStream_t stream) { return run_norm<T, false>(p, stream); }
 template <typename T> int run_to8(const Norm &p, hipStream_t stream) { return run_norm<T, true>(p, stream); }
@@ -390,12 +433,18 @@ int64_t groups_of(int64_t rows, int ty) { return std::max<int64_t>(1, std::min<i
 template <typename T>
 int run_grad(Grad p, float *dweight, float *workspace, hipStream_t stream)
 {
-    const Shape l = shape_of((p.width + Vec<T>::n - 1) / Vec<T>::n, 1, 4);
+    constexpr int n = Vec<T>::n;
+    const int64_t pieces = (p.width + n - 1) / n;
+    // two pieces on 256 lanes rather than one on 512 (8192 rows of 4096 bf16: 47 us and 65), which are for longer rows
+    const Shape l = shape_of(pieces, pieces > 2 * kThreads ? kMostLanes : kThreads, 2);
+    const bool held = pieces <= (int64_t)l.tx * l.hold;
     p.tx = l.tx;
-    const int64_t groups = groups_of(p.rows, kThreads / l.tx);
+    const int threads = std::max(l.tx, kThreads);
+    const int64_t groups = groups_of(p.rows, threads / l.tx);
     p.dw = !dweight ? nullptr : groups == 1 ? dweight : workspace;
-    auto *k = l.hold == 1 ? norm_grad<T, 1> : l.hold == 2 ? norm_grad<T, 2> : norm_grad<T, 4>;
-    if (int rc = launch("norm_grad launch", k, dim3((unsigned)groups), dim3(kThreads), stream, p)) return rc;
+    auto *k = p.width % n == 0 ? (l.hold == 1 ? norm_grad<T, 1, kWhole> : norm_grad<T, 2, kWhole>)
+              : p.width > n && held ? (l.hold == 1 ? norm_grad<T, 1, kOverlap> : norm_grad<T, 2, kOverlap>) : norm_grad<T, 1, kRest>;
+    if (int rc = launch("norm_grad launch", k, dim3((unsigned)groups), dim3(threads), stream, p)) return rc;
     if (!dweight || groups == 1) return OPEVO_OK;
     return launch("norm_grad_weight launch", norm_grad_weight, dim3((p.width + kCols - 1) / kCols), dim3(kCols * kLines), stream, workspace, (int)groups, p.width, dweight);
 }
