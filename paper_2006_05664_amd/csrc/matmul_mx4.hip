@@ -35,35 +35,15 @@ struct Product4 {
     bool odd;
 };
 
-// Sixteen rows of either operand, 128 values: lane l holds 32 values of row l % 16 and their factor, in byte SA (SB) of its scale word.
-template <int SB, int SA>
+// Sixteen rows of either operand, 128 values: lane l holds 32 values of row l % 16 and their factor, in byte BYTE of its factor word.
+template <int BYTE>
 __device__ __forceinline__ f32x4 mfma(i32x4 b, i32x4 a, f32x4 c, int sb, int sa)
 {
     const i32x8 b8 = {b[0], b[1], b[2], b[3], 0, 0, 0, 0}, a8 = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b8, a8, c, 4, 4, SB, sb, SA, sa);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b8, a8, c, 4, 4, BYTE, sb, BYTE, sa);
 }
-// The bytes are known once the loops around are unrolled.
-__device__ __forceinline__ f32x4 mfma_at(int at_b, int at_a, i32x4 b, i32x4 a, f32x4 c, int sb, int sa)
-{
-    switch (at_b * 4 + at_a) {
-    case 0: return mfma<0, 0>(b, a, c, sb, sa);
-    case 1: return mfma<0, 1>(b, a, c, sb, sa);
-    case 2: return mfma<0, 2>(b, a, c, sb, sa);
-    case 3: return mfma<0, 3>(b, a, c, sb, sa);
-    case 4: return mfma<1, 0>(b, a, c, sb, sa);
-    case 5: return mfma<1, 1>(b, a, c, sb, sa);
-    case 6: return mfma<1, 2>(b, a, c, sb, sa);
-    case 7: return mfma<1, 3>(b, a, c, sb, sa);
-    case 8: return mfma<2, 0>(b, a, c, sb, sa);
-    case 9: return mfma<2, 1>(b, a, c, sb, sa);
-    case 10: return mfma<2, 2>(b, a, c, sb, sa);
-    case 11: return mfma<2, 3>(b, a, c, sb, sa);
-    case 12: return mfma<3, 0>(b, a, c, sb, sa);
-    case 13: return mfma<3, 1>(b, a, c, sb, sa);
-    case 14: return mfma<3, 2>(b, a, c, sb, sa);
-    default: return mfma<3, 3>(b, a, c, sb, sa);
-    }
-}
+// The byte is known once the loops around are unrolled.
+__device__ __forceinline__ f32x4 mfma_at(int byte, i32x4 b, i32x4 a, f32x4 c, int sb, int sa) { return byte ? mfma<1>(b, a, c, sb, sa) : mfma<0>(b, a, c, sb, sa); }
 
 // Writes a wave's MI x NI atoms, rows r.first + m0 .. and columns col0 .. of C.  Lane l of an atom holds columns 4 * (l / 16) .. + 3 of row l % 16; the 16 rows of an atom row go through a
 // piece of LDS of the wave's own and leave as whole lines, 16 bytes a lane.
@@ -101,6 +81,14 @@ __device__ __forceinline__ void store_sums(const Product4 &p, const Rows &r, int
         }
         exchange();
     }
+}
+
+template <int MI, int NI>
+__device__ __forceinline__ void store_as(const Product4 &p, const Rows &r, int m0, int col0, const f32x4 (&acc)[MI][NI], int8_t *patch, int lane)
+{
+    if (p.out == OPEVO_F32) store_sums<float>(p, r, m0, col0, acc, patch, lane);
+    else if (p.out == OPEVO_BF16) store_sums<__bf16>(p, r, m0, col0, acc, patch, lane);
+    else store_sums<_Float16>(p, r, m0, col0, acc, patch, lane);
 }
 
 // ------------------------------------------------------------------ few rows
@@ -142,7 +130,7 @@ void product4_thin(Product4 p)
         };
         auto multiply = [&](const i32x4 (&of)[2][4], const i32x4 (&f)[2]) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) acc = mfma<0, 0>(of[1][u], of[0][u], acc, (int)((unsigned)f[1][u] >> 8 * g), (int)((unsigned)f[0][u] >> 8 * g));
+            for (int u = 0; u < 4; ++u) acc = mfma<0>(of[1][u], of[0][u], acc, (int)((unsigned)f[1][u] >> 8 * g), (int)((unsigned)f[0][u] >> 8 * g));
         };
         int s = wave;
         if (s < steps) load(v, fv, s);
@@ -195,38 +183,6 @@ __device__ __forceinline__ void load_word_to_lds(const int8_t *base, unsigned of
     const int8_t *copy;
     asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dword %1, %0" : "=&s"(copy) : "v"(off), "s"(base), "s"(lds) : "memory", "m0");
 }
-
-// Factors of N atoms for both steps of a slab, as the matrix instruction takes them.  Four atoms at a time: lane (r, g) reads the eight factors of row r of atom g, and the four lanes
-// of an r exchange bytes until each has its own group's factor of all four atoms in a word (byte i: atom i).  Fewer: every lane reads its row's word and shifts.
-template <int N> struct Factors {
-    static constexpr bool FOURS = N % 4 == 0;
-    static constexpr int W = FOURS ? N / 4 : N;
-    int raw[W][2], word[2][W];
-    // `at`: the factors of the wave's first row
-    __device__ __forceinline__ void read(const int8_t *at, int lane)
-    {
-#pragma unroll
-        for (int i = 0; i < W; ++i) __builtin_memcpy(raw[i], __builtin_assume_aligned(at + (FOURS ? (i * 4 + (lane >> 4)) * 16 + (lane & 15) : i * 16 + (lane & 15)) * 8, 8), 8);
-    }
-    __device__ __forceinline__ void turn(int kk, int lane)
-    {
-        const int g = lane >> 4;
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            if constexpr (FOURS) {
-                typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-                const u32x2 far = __builtin_amdgcn_permlane32_swap((unsigned)raw[i][kk], (unsigned)raw[i][kk], false, false);      // the words of lanes g & 1 and g | 2
-                const unsigned x = __builtin_amdgcn_perm(far.y, far.x, g & 2 ? 0x07060302u : 0x05040100u);        // of either the bytes of groups 0 and 1, or 2 and 3
-                const u32x2 near = __builtin_amdgcn_permlane16_swap(x, x, false, false);                           // those of an even and an odd g
-                word[kk][i] = (int)__builtin_amdgcn_perm(near.y, near.x, g & 1 ? 0x07030501u : 0x06020400u);
-            } else {
-                word[kk][i] = (int)((unsigned)raw[i][kk] >> 8 * g);
-            }
-        }
-    }
-    __device__ __forceinline__ int of(int kk, int i) const { return word[kk][FOURS ? i / 4 : i]; }
-    static constexpr int at(int i) { return FOURS ? i % 4 : 0; }
-};
 
 template <typename S>
 __global__ __launch_bounds__(S::NT)
@@ -356,15 +312,10 @@ void product4_tile(Product4 p)
             else if (S::STAGES > 2 && more) WAIT_LGKM_VMCNT((S::STAGES - 2) * ALL);
             else WAIT_LGKM_VMCNT(0);
         };
-        // fragments: lane l holds row l % 16, the 32 values from 32 * (l / 16) of a step of 128
-        const int sw = lane >> 1 & 7, fr = lane & 15;
-        Factors<MI> fa;
-        Factors<NI> fb;
-        auto read_factors = [&](int stage) {
-            const int8_t *at = ring + stage * S::STAGE + S::CODES;
-            fa.read(at + wm * MI * 128, lane);
-            fb.read(at + (BM + wn * NI * 16) * 8, lane);
-        };
+        // fragments: lane l holds row l % 16, and of the step kk the 32 values from 64 * (l / 16) + 32 kk on; both steps' factors in a word
+        const int sw = lane >> 1 & 7, fr = lane & 15, g = lane >> 4;
+        auto chunk_at = [&](int stage, int kk) { return ring + stage * S::STAGE + ((g * 2 + kk ^ sw) << 4); };
+        auto read_factor = [&](int stage, int row) { return (int)*(const uint16_t *)(ring + stage * S::STAGE + S::CODES + (row + fr) * 8 + g * 2); };
         // prologue: slabs 0 .. STAGES - 1 under way, slab 0 landed, its first fragments read
         if (!S::DIRECT) {
             if (is_whole(0)) fetch(0);
@@ -377,14 +328,18 @@ void product4_tile(Product4 p)
         else if (S::STAGES > 2 && steps > S::STAGES) WAIT_LGKM_VMCNT((S::STAGES - 1) * ALL);
         else WAIT_LGKM_VMCNT(0);
         BARRIER();
-        read_factors(0);
         if constexpr (MI * NI <= 4) {
             // Few MFMAs a slab: the fragments of a whole slab are read at once, while the slab before it is multiplied.
             i32x4 ag[2][2][MI], bg[2][2][NI];
+            int fa[2][MI], fb[2][NI];
             auto read_slab = [&](int set, int stage) {
 #pragma unroll
+                for (int i = 0; i < MI; ++i) fa[set][i] = read_factor(stage, (wm * MI + i) * 16);
+#pragma unroll
+                for (int i = 0; i < NI; ++i) fb[set][i] = read_factor(stage, BM + (wn * NI + i) * 16);
+#pragma unroll
                 for (int kk = 0; kk < 2; ++kk) {
-                    const int8_t *at = ring + stage * S::STAGE + (((kk * 4 + (lane >> 4)) ^ sw) << 4);
+                    const int8_t *at = chunk_at(stage, kk);
 #pragma unroll
                     for (int i = 0; i < NI; ++i) bg[set][kk][i] = *(const i32x4 *)(at + BM * BK + (wn * NI * 16 + i * 16 + fr) * BK);
 #pragma unroll
@@ -398,9 +353,6 @@ void product4_tile(Product4 p)
                 const bool more = q + S::STAGES < steps;
                 wait_next(more);
                 BARRIER();                  // every wave has read slab q, and slab q + 1 has landed
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk) { fa.turn(kk, lane); fb.turn(kk, lane); }
-                read_factors(next);
                 read_slab(set ^ 1, next);
                 refill(how, q + S::STAGES, stage);
                 __builtin_amdgcn_sched_barrier(0);
@@ -409,7 +361,7 @@ void product4_tile(Product4 p)
 #pragma unroll
                     for (int m = 0; m < MI * NI; ++m) {
                         const int i = m / NI, j = m % NI;
-                        acc[i][j] = mfma_at(fb.at(j), fa.at(i), bg[set][kk][j], ag[set][kk][i], acc[i][j], fb.of(kk, j), fa.of(kk, i));
+                        acc[i][j] = mfma_at(kk, bg[set][kk][j], ag[set][kk][i], acc[i][j], fb[set][j], fa[set][i]);
                     }
                 stage = next;
             };
@@ -429,15 +381,21 @@ void product4_tile(Product4 p)
         constexpr int D = MI == 8 ? 3 : MI, R = MI == 8 ? 4 : 2 * MI, LAST = 2 * MI - D;
         static_assert(2 * MI % R == 0 && D < R && LAST >= MI && MI >= NI && D * NI > NI, "");
         i32x4 af[R], bf[2][NI];
-        auto chunk_at = [&](int stage, int kk) { return ring + stage * S::STAGE + (((kk * 4 + (lane >> 4)) ^ sw) << 4); };
+        int fa[MI], fb[NI], fb_next[NI];    // A's are read for the next slab as this one is done with them, B's are needed to its end
         auto read_a = [&](int stage, int f) { af[f % R] = *(const i32x4 *)(chunk_at(stage, f / MI) + (wm * MI * 16 + f % MI * 16 + fr) * BK); };
         auto read_b = [&](int stage, int kk, int i) { bf[kk][i] = *(const i32x4 *)(chunk_at(stage, kk) + BM * BK + (wn * NI * 16 + i * 16 + fr) * BK); };
+        auto read_fa = [&](int stage, int i) { fa[i] = read_factor(stage, (wm * MI + i) * 16); };
+        auto read_fb = [&](int (&to)[NI], int stage) {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) to[i] = read_factor(stage, BM + (wn * NI + i) * 16);
+        };
 #pragma unroll
         for (int i = 0; i < NI; ++i) read_b(0, 0, i);
 #pragma unroll
         for (int f = 0; f < D; ++f) read_a(0, f);
-        fa.turn(0, lane);
-        fb.turn(0, lane);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) read_fa(0, i);
+        read_fb(fb, 0);
         // Behind the first MFMA of fragment LAST every wave has read the slab and the next one has landed: its factors and first fragments are read and the stage is refilled.  (After
         // the last slab the reads fetch what the ring holds; nothing uses it.)
         int stage = 0;
@@ -449,22 +407,25 @@ void product4_tile(Product4 p)
                 const int kk = f / MI, x = f % MI;
 #pragma unroll
                 for (int y = 0; y < NI; ++y) {
-                    acc[x][y] = mfma_at(fb.at(y), fa.at(x), bf[kk][y], af[f % R], acc[x][y], fb.of(kk, y), fa.of(kk, x));
+                    acc[x][y] = mfma_at(kk, bf[kk][y], af[f % R], acc[x][y], fb[y], fa[x]);
                     if (f == LAST && y == 0) {
                         wait_next(more);
                         BARRIER();
-                        read_factors(next);
+                        read_fb(fb_next, next);
                         if constexpr (decltype(how)::value == kWhole) refill(how, q + S::STAGES, stage);
                     }
                     if (y == 0) read_a(f + D < 2 * MI ? stage : next, (f + D) % (2 * MI));
                     if (y == 1 && f < NI) read_b(stage, 1, f);
                     const int past = (f - LAST) * NI + y - 1;
                     if (past >= 0 && past < NI) read_b(next, 0, past);
-                    if (f == 0 && y == NI - 1) { fa.turn(1, lane); fb.turn(1, lane); }
-                    if (f == 2 * MI - 1 && y == NI - 1) { fa.turn(0, lane); fb.turn(0, lane); }
+                    if (f >= LAST && y == NI - 1)
+#pragma unroll
+                        for (int i = f == LAST ? 0 : x; i <= x; ++i) read_fa(next, i);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
+#pragma unroll
+            for (int i = 0; i < NI; ++i) fb[i] = fb_next[i];
             if constexpr (decltype(how)::value == kAny) {
 #pragma unroll
                 for (int m = 0; m < MI * NI; ++m) asm volatile("" : "+v"(acc[m / NI][m % NI]));      // the sums are due here
@@ -498,11 +459,162 @@ void product4_tile(Product4 p)
         __syncthreads();
         if (group > 0) return;
     }
-    int8_t *const patch = whole + wave * kPatch<float, NI>;
-    if (p.out == OPEVO_F32) store_sums<float>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch, lane);
-    else if (p.out == OPEVO_BF16) store_sums<__bf16>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch, lane);
-    else store_sums<_Float16>(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, patch, lane);
+    store_as(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, whole + wave * kPatch<float, NI>, lane);
 }
+
+// ------------------------------------------------------------------ tiles of long rows
+// The same for operands that can come straight to LDS and whose K is a multiple of 1024, so that nothing is ragged.  The factors come for four slabs at a time, 32 bytes a row, two sets in turn:
+// eight bytes a row with every slab take as many requests as the codes, and cost 8192^3 some 40 us.  A set stands as two halves of [rows][16] bytes, each for two slabs.
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
+struct LongShape {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, BK = 128, ROWS = BM + BN;
+    static constexpr int NW = WM * WN, NT = NW * 64, MI = BM / WM / 16, NI = BN / WN / 16;
+    static constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, PER = LA + LB, STAGE = ROWS * BK;
+    static constexpr int SET = ROWS * 32, PIECES = ROWS * 2 / 64, FPER = PIECES / NW, BYTES = STAGES * STAGE + 2 * SET;
+    // two slabs at least lie between a set's loads and its first use, and no more than two slabs' loads are on their way behind them when they are waited for
+    static_assert(MI * WM * 16 == BM && NI * WN * 16 == BN && LA * 8 * NW == BM && LB * 8 * NW == BN && FPER * NW == PIECES && BM % 64 == 0 && (STAGES == 2 || STAGES == 4) && MI >= NI
+                      && BYTES <= 160 * 1024 && NW * kPatch<float, NI> <= BYTES,
+                  "");
+};
+
+#define LDS(T) const __attribute__((address_space(3))) T *
+template <typename S>
+__global__ __launch_bounds__(S::NT)
+void product4_long(Product4 p)
+{
+    constexpr int BM = S::BM, BN = S::BN, BK = S::BK, MI = S::MI, NI = S::NI, LA = S::LA, LB = S::LB, PER = S::PER, ROWS = S::ROWS;
+    __shared__ __attribute__((aligned(1024))) int8_t ring[S::BYTES];
+    Rows r;
+    if (!find_rows(p, BM, row_tile(), &r)) return;
+    r.first = (long)uniform((const int8_t *)r.first);           // alike for all lanes, which the compiler does not see: they would take vector registers to the end
+    r.last = (long)uniform((const int8_t *)r.last);
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wm = wave / S::WN, wn = wave % S::WN, n0 = blockIdx.x * BN;
+    f32x4 acc[MI][NI] = {};
+    if (!r.zero) {
+        const unsigned ring_at = uniform((int)(unsigned)(unsigned long)(__attribute__((address_space(3))) int8_t *)ring), sets_at = ring_at + S::STAGES * S::STAGE;
+        const int rows = (int)(r.last - r.first), cols = p.n - n0, steps = p.k / BK;
+        const long b0 = (long)r.expert * p.n + n0;
+        // this wave's pieces of a slab: eight rows each, lane -> row lane / 8, chunk position lane % 8; and of a set: 64 rows of a half each
+        unsigned off[PER], foff[S::FPER];
+#pragma unroll
+        for (int t = 0; t < PER; ++t) {
+            const bool is_a = t < LA;
+            const int row = (is_a ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8;
+            off[t] = (unsigned)min(row, (is_a ? rows : cols) - 1) * (unsigned)(is_a ? p.lda : p.ldb);
+            asm("" : "+v"(off[t]));         // product and sum in one instruction would take, and keep, two registers
+            off[t] += ((lane & 7) ^ (row >> 1 & 7)) * 16;
+        }
+        int half[S::FPER], first[S::FPER];
+#pragma unroll
+        for (int t = 0; t < S::FPER; ++t) {
+            const int piece = wave * S::FPER + t, row = piece % (ROWS / 64) * 64 + lane;
+            half[t] = piece / (ROWS / 64);
+            first[t] = piece % (ROWS / 64) * 64;
+            foff[t] = first[t] < BM ? (unsigned)min(row, rows - 1) * (unsigned)p.ldsa : (unsigned)min(row - BM, cols - 1) * (unsigned)p.ldsb;
+        }
+        const int8_t *abase = uniform((const int8_t *)p.a + r.first * p.lda), *bbase = uniform((const int8_t *)p.b + b0 * p.ldb);
+        const int8_t *afact = uniform((const int8_t *)p.sa + r.first * p.ldsa), *bfact = uniform((const int8_t *)p.sb + b0 * p.ldsb);
+        auto issue = [&](int step, int stage) {
+            const int8_t *as = abase + (long)step * BK, *bs = bbase + (long)step * BK;
+            const unsigned at = ring_at + stage * S::STAGE, at_a = at + wave * LA * 1024, at_b = at + BM * BK + wave * LB * 1024;
+#pragma unroll
+            for (int t = 0; t < PER; ++t) load_to_lds(t < LA ? as : bs, off[t], t < LA ? at_a + t * 1024 : at_b + (t - LA) * 1024);
+        };
+        // Nothing counts these loads: waits for so many slabs in flight wait for them as well, as they are older.
+        auto issue_set = [&](int set) {
+#pragma unroll
+            for (int t = 0; t < S::FPER; ++t)
+                load_to_lds(uniform((first[t] < BM ? afact : bfact) + (long)set * 32 + half[t] * 16), foff[t], sets_at + (set & 1) * S::SET + half[t] * (ROWS * 16) + first[t] * 16);
+        };
+        // fragments: lane l holds row l % 16, and of the step kk the 32 values from 64 * (l / 16) + 32 kk on; both steps' factors in a word
+        constexpr int D = MI == 8 ? 3 : MI, R = MI == 8 ? 4 : 2 * MI, LAST = 2 * MI - D;
+        static_assert(2 * MI % R == 0 && D < R && LAST >= MI && D * NI > NI, "");
+        // Where they stand, as LDS addresses that go on from slab to slab: A's and B's of either step, and the factors.
+        static_assert((S::STAGES & (S::STAGES - 1)) == 0 && (S::STAGE & (S::STAGE - 1)) == 0 && (S::SET & (S::SET - 1)) == 0, "stages and sets differ in a bit of the address");
+        const int sw = lane >> 1 & 7, fr = lane & 15, g = lane >> 4;
+        unsigned at_a[2], at_b[2], at_fa = sets_at + (wm * MI * 16 + fr) * 16 + g * 2, at_fb = sets_at + (BM + wn * NI * 16 + fr) * 16 + g * 2;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            at_a[kk] = ring_at + (wm * MI * 16 + fr) * BK + ((g * 2 + kk ^ sw) << 4);
+            at_b[kk] = ring_at + (BM + wn * NI * 16 + fr) * BK + ((g * 2 + kk ^ sw) << 4);
+        }
+        i32x4 af[R], bf[2][NI];
+        int fa[MI], fb[2][NI];
+        auto read_a = [&](int f) { af[f % R] = *(LDS(i32x4))(at_a[f / MI] + f % MI * 16 * BK); };
+        auto read_b = [&](int kk, int i) { bf[kk][i] = *(LDS(i32x4))(at_b[kk] + i * 16 * BK); };
+        auto factor_at = [&](unsigned at, int j, int i) { return (int)*(LDS(uint16_t))(at + j / 2 * (ROWS * 16) + j % 2 * 8 + i * 256); };
+        issue_set(0);
+#pragma unroll
+        for (int s = 0; s < S::STAGES; ++s) issue(s, s);        // there are four slabs at least
+        if (S::STAGES > 2) WAIT_LGKM_VMCNT((S::STAGES - 1) * PER);
+        else WAIT_LGKM_VMCNT(0);
+        BARRIER();
+#pragma unroll
+        for (int i = 0; i < NI; ++i) read_b(0, i);
+#pragma unroll
+        for (int f = 0; f < D; ++f) read_a(f);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fa[i] = factor_at(at_fa, 0, i);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) fb[0][i] = factor_at(at_fb, 0, i);
+        // Slab j of a set, as in product4_tile.
+        auto slab = [&](auto at, auto last, int q) {
+            constexpr int J = decltype(at)::value;
+            constexpr bool MORE = !decltype(last)::value || J < 3, REFILL = !decltype(last)::value || J + S::STAGES < 4, AFTER = !decltype(last)::value || J + S::STAGES - 1 < 4;
+#pragma unroll
+            for (int f = 0; f < 2 * MI; ++f) {
+                const int kk = f / MI, x = f % MI;
+#pragma unroll
+                for (int y = 0; y < NI; ++y) {
+                    acc[x][y] = mfma_at(kk, bf[kk][y], af[f % R], acc[x][y], fb[J & 1][y], fa[x]);
+                    if (MORE && f == LAST && y == 0) {
+                        if (S::STAGES > 2 && AFTER) WAIT_LGKM_VMCNT((S::STAGES - 2) * PER);
+                        else WAIT_LGKM_VMCNT(0);
+                        BARRIER();
+                        // on to the next stage, and set (the compiler is not to keep an address for each)
+                        constexpr unsigned flip = ((J + 1) % S::STAGES ^ J % S::STAGES) * S::STAGE;
+#pragma unroll
+                        for (int o = 0; o < 2; ++o) {
+                            at_a[o] ^= flip;
+                            at_b[o] ^= flip;
+                            asm("" : "+v"(at_a[o]), "+v"(at_b[o]));
+                        }
+                        if (J == 3) {
+                            at_fa ^= S::SET;
+                            at_fb ^= S::SET;
+                        }
+                        asm("" : "+v"(at_fa), "+v"(at_fb));
+#pragma unroll
+                        for (int i = 0; i < NI; ++i) fb[(J + 1) & 1][i] = factor_at(at_fb, (J + 1) % 4, i);
+                        if constexpr (REFILL) issue(q + J + S::STAGES, J % S::STAGES);
+                        if constexpr (J == 0 && !decltype(last)::value) issue_set(q / 4 + 1);
+                    }
+                    if (y == 0 && (MORE || f + D < 2 * MI)) read_a((f + D) % (2 * MI));
+                    if (y == 1 && f < NI) read_b(1, f);
+                    const int past = (f - LAST) * NI + y - 1;
+                    if (MORE && past >= 0 && past < NI) read_b(0, past);
+                    if (MORE && f >= LAST && y == NI - 1)
+#pragma unroll
+                        for (int i = f == LAST ? 0 : x; i <= x; ++i) fa[i] = factor_at(at_fa, (J + 1) % 4, i);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        };
+        auto four = [&](auto last, int q) {
+            slab(std::integral_constant<int, 0>(), last, q);
+            slab(std::integral_constant<int, 1>(), last, q);
+            slab(std::integral_constant<int, 2>(), last, q);
+            slab(std::integral_constant<int, 3>(), last, q);
+        };
+        int q = 0;
+        for (; q + 4 < steps; q += 4) four(std::false_type(), q);
+        four(std::true_type(), q);
+        WAIT_LGKM_VMCNT(0);
+    }
+    __syncthreads();
+    store_as(p, r, wm * MI * 16, n0 + wn * NI * 16, acc, ring + wave * kPatch<float, NI>, lane);
+}
+
 
 using opevo::launch;
 
@@ -521,6 +633,12 @@ int run_tile(const Product4 &p, hipStream_t stream)
     return launch("product4 launch", product4_tile<S>, grid_of(p, S::BM, S::BN), dim3(S::NT), stream, p);
 }
 
+template <typename S>
+int run_long(const Product4 &p, hipStream_t stream)
+{
+    return launch("product4 launch", product4_long<S>, grid_of(p, S::BM, S::BN), dim3(S::NT), stream, p);
+}
+
 template <int W>
 int run_thin(const Product4 &p, hipStream_t stream)
 {
@@ -529,7 +647,9 @@ int run_thin(const Product4 &p, hipStream_t stream)
 
 // A kernel and what it takes, in us: launch + max(steps * chain, load * (tile + steps * rate)), where steps is how many slabs (thin: steps of 256 bytes) a wave
 // goes through and load the workgroups for each of the 256 compute units, rounded up where that foretold the times better.  The first term is a workgroup's chain of latencies,
-// the second what a compute unit gets through.
+// the second what a compute unit gets through.  The constants were fitted to the times of every kernel at 750 random sizes of 1 - 8192 rows, 64 - 8192 columns and K of 64 - 8192 (a third
+// each of K in multiples of 1024, of 32, and any), those near the best one's counting most; the kernel chosen by them took 1.5, 3.5 and 1.7 % more than the best of all
+// in the geometric mean, at most 1.9 times as much.  By experts they are used with the tiles that an even deal of the rows would make.
 struct Kernel {
     int (*run)(const Product4 &, hipStream_t);
     int bm, bn, step, ways;             // tile, bytes of a step, waves or groups that share the steps
@@ -538,18 +658,28 @@ struct Kernel {
     float launch, chain, tile, rate;
 };
 constexpr int64_t kAll = INT64_MAX;
+const Kernel kLong[] = {                // besides those of kDirect
+    {run_long<LongShape<256, 256, 2, 4, 2>>, 256, 256, 128, 1, kAll, false, 6.81f, 1.43f, 5.13f, 2.32f},
+    {run_long<LongShape<128, 128, 2, 2, 2>>, 128, 128, 128, 1, kAll, false, 4.12f, 0.561f, 1.83f, 0.686f},
+    {run_long<LongShape<128, 128, 2, 4, 4>>, 128, 128, 128, 1, kAll, false, 3.59f, 0.546f, 2.08f, 0.889f},
+};
 const Kernel kDirect[] = {
-    {run_tile<Shape<true, 256, 256, 2, 4, 2>>, 256, 256, 128, 1, kAll, true, 0.f, 1.6f, 10.8f, 1.41f},
-    {run_tile<Shape<true, 128, 128, 2, 4, 4>>, 128, 128, 128, 1, kAll, true, 0.f, 0.f, 5.18f, 0.576f},
-    {run_tile<Shape<true, 64, 64, 2, 4, 4>>, 64, 64, 128, 1, kAll, false, 2.6f, 0.322f, 0.783f, 0.322f},
-    {run_tile<Shape<true, 32, 32, 2, 2, 6, 2>>, 32, 32, 128, 2, kAll, false, 2.39f, 0.26f, 0.532f, 0.372f},
-    {run_thin<4>, 16, 16, 256, 4, 256, false, 2.22f, 0.683f, 0.f, 0.775f},
+    {run_tile<Shape<true, 256, 256, 2, 4, 2>>, 256, 256, 128, 1, kAll, false, 5.94f, 1.89f, 7.01f, 2.67f},
+    {run_tile<Shape<true, 128, 128, 2, 2, 2>>, 128, 128, 128, 1, kAll, false, 4.4f, 0.938f, 1.75f, 0.971f},
+    {run_tile<Shape<true, 128, 128, 2, 4, 4>>, 128, 128, 128, 1, kAll, false, 3.82f, 0.745f, 2.54f, 1.07f},
+    {run_tile<Shape<true, 128, 64, 4, 2, 3>>, 128, 64, 128, 1, kAll, true, 0.566f, 0.699f, 2.99f, 0.55f},
+    {run_tile<Shape<true, 64, 64, 2, 2, 4>>, 64, 64, 128, 1, kAll, true, 2.46f, 0.356f, 0.881f, 0.319f},
+    {run_tile<Shape<true, 32, 64, 1, 4, 4, 2>>, 32, 64, 128, 2, kAll, true, 1.13f, 0.556f, 2.18f, 0.469f},
+    {run_tile<Shape<true, 32, 32, 2, 2, 6, 2>>, 32, 32, 128, 2, kAll, true, 1.38f, 0.469f, 1.78f, 0.35f},
+    {run_thin<4>, 16, 16, 256, 4, 300, true, 2.63f, 0.778f, 0.f, 0.605f},
 };
 const Kernel kAny[] = {
-    {run_tile<Shape<false, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, kAll, true, 0.f, 0.f, 4.32f, 0.78f},
-    {run_tile<Shape<false, 64, 64, 2, 4, 2>>, 64, 64, 128, 1, kAll, true, 2.07f, 0.466f, 1.25f, 0.461f},
-    {run_tile<Shape<false, 32, 32, 2, 2, 2, 2>>, 32, 32, 128, 2, kAll, true, 2.4f, 0.545f, 0.501f, 0.363f},
-    {run_thin<4>, 16, 16, 256, 4, 64, true, 0.993f, 2.07f, 0.f, 1.74f},
+    {run_tile<Shape<false, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, kAll, true, 0.368f, 1.48f, 4.3f, 1.18f},
+    {run_tile<Shape<false, 128, 64, 4, 2, 2>>, 128, 64, 128, 1, kAll, true, 0.773f, 1.13f, 3.44f, 0.857f},
+    {run_tile<Shape<false, 64, 64, 2, 4, 2>>, 64, 64, 128, 1, kAll, true, 1.08f, 0.711f, 2.49f, 0.616f},
+    {run_tile<Shape<false, 32, 64, 1, 4, 2, 2>>, 32, 64, 128, 2, kAll, true, 1.25f, 0.913f, 2.75f, 0.778f},
+    {run_tile<Shape<false, 32, 32, 2, 2, 2, 2>>, 32, 32, 128, 2, kAll, true, 2.68f, 0.447f, 0.891f, 0.51f},
+    {run_thin<4>, 16, 16, 256, 4, 300, true, 2.29f, 1.87f, 0.f, 1.09f},
 };
 
 int run_product4(const Product4 &p, hipStream_t stream)
@@ -570,6 +700,7 @@ int run_product4(const Product4 &p, hipStream_t stream)
         const float us = k.launch + std::max(steps * k.chain, load * (k.tile + steps * k.rate));
         if (!best || us < least) { best = &k; least = us; }
     };
+    if (direct && p.k % (4 * 128) == 0) for (const Kernel &k : kLong) consider(k);
     if (direct) for (const Kernel &k : kDirect) consider(k);
     else for (const Kernel &k : kAny) consider(k);
     return best->run(p, stream);
