@@ -45,7 +45,7 @@ struct Layer {
     void *y;
     long ld_y;
     Plan *plan;
-    __bf16 *h;                          // [held slots][parts][ld_h]
+    __bf16 *h;                          // [held slots][parts][ld_h], zeros from `inner` on
     long ld_h;
 };
 
@@ -66,6 +66,7 @@ struct Weights8 {
     const uint8_t *row;
     int k;
     __device__ __forceinline__ void at(const uint8_t *w, long ld, const void *, long, long n, int k_) { row = w + n * ld; k = k_; }
+    __device__ __forceinline__ void skip(int values) { row += values; }
     __device__ __forceinline__ void load(Raw &r, int k0, int g) const
     {
         __builtin_memcpy(&r.v[0], row + k0 + g * 32, 16);
@@ -95,6 +96,11 @@ struct Weights4 {
     const uint8_t *row, *by;
     int k;                              // values
     __device__ __forceinline__ void at(const uint8_t *w, long ld, const void *s, long ld_s, long n, int k_) { row = w + n * ld; by = (const uint8_t *)s + n * ld_s; k = k_; }
+    __device__ __forceinline__ void skip(int values)
+    {
+        row += values / 2;
+        by += values / 32;
+    }
     __device__ __forceinline__ void load(Raw &r, int k0, int g) const
     {
         __builtin_memcpy(&r.f, by + k0 / 32, 8);
@@ -126,6 +132,10 @@ template <typename T> struct Parts { static constexpr int n = 1, h = 2; };
 template <> struct Parts<_Float16> { static constexpr int n = 2, h = 2; };
 template <> struct Parts<float> { static constexpr int n = 3, h = 3; };
 
+// Where value c of a row of h stands: the eight values that a lane takes of it at a time stand side by side with those that the lanes of the other three groups take at the same time, so that an
+// access of the second launch is 64 contiguous bytes a row and not 16 of every 64.
+__device__ __forceinline__ int place_in_h(int c) { return c / kStep * kStep + c % 32 / 8 * 32 + c % kStep / 32 * 8 + c % 8; }
+
 template <typename T> __device__ __forceinline__ bf16x8 operand(const T (&v)[8], int part)
 {
     if constexpr (Parts<T>::n == 1) {
@@ -146,20 +156,26 @@ template <typename T> __device__ __forceinline__ bf16x8 operand(const T (&v)[8],
     }
 }
 
-// A lane's row of activations.  A lane without one takes any: a column of the product is its row's alone.
-template <typename T, int SUB> struct Activations {
+// A lane's row of activations.  A lane without one (`on` is false) loads nothing and multiplies what its registers hold: a column of the product is its row's alone.  (Loading some row instead
+// costs as much as a row of its own: 32 tokens x 4 of 4096 x 1024, second launch, 49 us instead of 42.)
+// ORDERED: values as place_in_h puts them, rows without a ragged end.
+template <typename T, int SUB, bool ORDERED> struct Activations {
     struct Raw { T v[SUB][4][8]; };
     const T *row;
     int part, k;
+    bool on;
     __device__ __forceinline__ void load(Raw &r, int k0, int g) const
     {
+        if (!on) return;
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) __builtin_memcpy(r.v[u][j], row + k0 + u * kStep + g * 32 + j * 8, sizeof r.v[u][j]);
+            for (int j = 0; j < 4; ++j) __builtin_memcpy(r.v[u][j], row + k0 + u * kStep + (ORDERED ? j * 32 + g * 8 : g * 32 + j * 8), sizeof r.v[u][j]);
     }
     __device__ __forceinline__ void load_ragged(Raw &r, int k0, int g) const
     {
+        if (ORDERED) return load(r, k0, g);
+        if (!on) return;
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -175,12 +191,12 @@ template <typename T, int SUB> struct Activations {
 
 // The iterations first, first + stride, ... along K, the last one of which may be ragged; the wave whose turn it is takes that one.  The weights of the next iteration come from memory meanwhile; the
 // activations, of the same one, from the caches: they are asked for first, because loads are waited for in their order.
-template <bool RAGGED, typename Q, typename T, int NI>
-__device__ __forceinline__ void multiply(const Q (&w)[NI], const Activations<T, Q::SUB> &x, int first, int stride, int g, f32x4 (&acc)[NI])
+template <bool RAGGED, bool ORDERED, typename Q, typename T, int NI>
+__device__ __forceinline__ void multiply(const Q (&w)[NI], const Activations<T, Q::SUB, ORDERED> &x, int first, int stride, int g, f32x4 (&acc)[NI])
 {
     constexpr int LONG = Q::SUB * kStep;
     typedef typename Q::Raw W;
-    typedef typename Activations<T, Q::SUB>::Raw X;
+    typedef typename Activations<T, Q::SUB, ORDERED>::Raw X;
     const int whole = x.k / LONG;
     auto load = [&](W (&wr)[NI], int it) {
 #pragma unroll
@@ -285,7 +301,7 @@ __device__ __forceinline__ int expert_at(const unsigned *words, int index, int l
 // h of an expert's rows for 16 * NP of its inner channels: gate and up, NP tiles of 16 rows of weights each.  The W waves deal the iterations along K among themselves.  NP is 2, so that the operands of
 // the activations serve four tiles, and 1 where K ends inside an iteration: the ragged loads would not leave registers for more.
 template <typename T, typename Q, int W, bool RAGGED>
-__global__ __launch_bounds__(W * 64, 2)
+__global__ __launch_bounds__(W * 64, RAGGED && Parts<T>::n == 3 ? 1 : 2)
 void layer_in(Layer p)
 {
     constexpr int NT = W * 64, NP = RAGGED ? 1 : 2, NI = 2 * NP, PX = Parts<T>::n, PH = Parts<T>::h, PER = 16 / PX;
@@ -298,7 +314,7 @@ void layer_in(Layer p)
         if (blockIdx.x == 0) write_plan<NT>(p, ids, words);
         return;
     }
-    const int e = expert_at(words, blockIdx.y, lane);
+    const int e = expert_at(words, blockIdx.y, lane), c0 = blockIdx.x * (NP * 16);
     if (e < 0) return;                      // alike for the workgroup
     int base = 0, rows = 0;
     for (int s0 = 0; s0 < p.slots; s0 += 64) {
@@ -309,25 +325,31 @@ void layer_in(Layer p)
         rows += __popcll(same);
     }
     __syncthreads();
-    const int c0 = blockIdx.x * (NP * 16);
     const long first = (long)e * 2 * p.inner;
     Q w[NI];
 #pragma unroll
     for (int n = 0; n < NI; ++n) w[n].at(p.win, p.ld_in, p.sin, p.ld_sin, first + (n < NP ? 0 : p.inner) + min(c0 + n % NP * 16 + r, p.inner - 1), p.width);
     for (int t0 = 0; t0 < rows; t0 += PER) {
-        Activations<T, Q::SUB> x;
+        Activations<T, Q::SUB, false> x;
+        x.on = r < PER * PX && t0 + r / PX < rows;
         x.row = (const T *)p.x + list[min(t0 + r / PX, rows - 1)] / p.k * p.ld_x;
         x.part = r % PX;
         x.k = p.width;
         f32x4 acc[NI] = {};
-        multiply<RAGGED, Q, T, NI>(w, x, wave, W, g, acc);
+        multiply<RAGGED, false, Q, T, NI>(w, x, wave, W, g, acc);
 #pragma unroll
         for (int n = 0; n < NI; ++n) sums[wave][n][lane] = acc[n];
         __syncthreads();
         // an output a thread: one inner channel of one row
         for (int o = threadIdx.x; o < PER * NP * 16; o += NT) {
             const int c = o % (NP * 16), at = o / (NP * 16), row = t0 + at;
-            if (row >= rows || c0 + c >= p.inner) continue;
+            if (row >= rows || c0 + c >= p.ld_h) continue;
+            __bf16 *to = p.h + (long)(base + row) * PH * p.ld_h + place_in_h(c0 + c);
+            if (c0 + c >= p.inner) {
+#pragma unroll
+                for (int part = 0; part < PH; ++part) to[part * p.ld_h] = (__bf16)0.f;
+                continue;
+            }
             float v[2] = {0.f, 0.f};
 #pragma unroll
             for (int side = 0; side < 2; ++side)
@@ -336,7 +358,6 @@ void layer_in(Layer p)
                     for (int o = 0; o < W; ++o) v[side] += ((const float *)&sums[o][side * NP + c / 16][c % 16 / 4 * 16 + at * PX + part])[c % 4];
             const float gate = v[0] * Q::scale(p.sin, first + c0 + c), up = v[1] * Q::scale(p.sin, first + p.inner + c0 + c);
             const float h = gate / (1.f + expf(-gate)) * up, second = rest(h);
-            __bf16 *to = p.h + (long)(base + row) * PH * p.ld_h + c0 + c;
             to[0] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(h) >> 16));
             if constexpr (PH == 2) to[p.ld_h] = (__bf16)second;
             else {
@@ -349,18 +370,21 @@ void layer_in(Layer p)
 }
 
 // ------------------------------------------------------------------ the second launch
-// y of 16 columns for all tokens: a task is an expert in use and a share of K, the W waves deal the tasks among themselves, what they find for each row meets in LDS, and the rows of a
-// token are added up there in the order of its slots.
+// y of COLS = 16 / S columns for all tokens: a task is an expert in use and a share of K, the W waves deal the tasks among themselves, what they find for each row meets in LDS, and the rows of
+// a token are added up there in the order of its slots.
+// S > 1, for few tokens and few columns: K falls into S parts, and the 16 rows of weights of a product are COLS columns in each of the parts, the 16 rows of h COLS rows in each of
+// them.  Of the product the S blocks of a part with itself are used; a wave reads as much as ever, and there are S times as many workgroups.
 constexpr int kShares = 1024;           // rows of 16 sums in the LDS
 
-template <typename T, typename Q, int W, bool RAGGED>
+template <typename T, typename Q, int W, int S, bool RAGGED>
 __global__ __launch_bounds__(W * 64)
 void layer_out(Layer p)
 {
-    constexpr int NT = W * 64, PH = Parts<T>::h, PER = 16 / PH;
-    __shared__ int expert[kMaxSlots], start[kMaxSlots + 1], place[kMaxSlots];
-    __shared__ __attribute__((aligned(16))) float z[kShares][16];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15, n0 = blockIdx.x * 16;
+    constexpr int NT = W * 64, COLS = 16 / S, PH = Parts<T>::h, PER = COLS / PH;
+    static_assert(PER >= 1 && (S == 1 || !RAGGED), "");
+    __shared__ int expert[kMaxSlots], start[kMaxSlots], place[kMaxSlots];
+    __shared__ __attribute__((aligned(16))) float z[kShares * S][COLS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15, part = r / COLS, c = r % COLS, n0 = blockIdx.x * COLS;
     for (int s = threadIdx.x; s < p.slots; s += NT) {
         expert[s] = p.plan->expert[s];
         start[s] = p.plan->start[s];
@@ -368,7 +392,7 @@ void layer_out(Layer p)
     }
     const int active = __builtin_amdgcn_readfirstlane(p.plan->active), held = __builtin_amdgcn_readfirstlane(p.plan->held);
     __syncthreads();
-    const int count = (p.inner + Q::SUB * kStep - 1) / (Q::SUB * kStep);
+    const int length = p.inner / S, count = (length + Q::SUB * kStep - 1) / (Q::SUB * kStep);
     // shares of K: as many as make the waves' iterations fewest, two lost to each task's start
     int shares = 1, least = INT32_MAX;
     for (int s = 1; s <= W && s <= count && s * held <= kShares; s *= 2) {
@@ -381,40 +405,43 @@ void layer_out(Layer p)
         const int e = __builtin_amdgcn_readfirstlane(expert[index]), base = __builtin_amdgcn_readfirstlane(start[index]),
                   rows = (index + 1 < active ? __builtin_amdgcn_readfirstlane(start[index + 1]) : held) - base;
         Q w[1];
-        w[0].at(p.wout, p.ld_out, p.sout, p.ld_sout, (long)e * p.width + min(n0 + r, p.width - 1), p.inner);
+        w[0].at(p.wout, p.ld_out, p.sout, p.ld_sout, (long)e * p.width + min(n0 + c, p.width - 1), p.inner);
+        if (S > 1) w[0].skip(part * length);
         for (int t0 = 0; t0 < rows; t0 += PER) {
-            const int at = t0 + r / PH;
-            Activations<__bf16, Q::SUB> x;
-            x.row = p.h + ((long)(base + min(at, rows - 1)) * PH + r % PH) * p.ld_h;
+            const int at = t0 + c / PH;
+            Activations<__bf16, Q::SUB, true> x;
+            x.on = c < PER * PH && at < rows;
+            x.row = p.h + ((long)(base + min(at, rows - 1)) * PH + c % PH) * p.ld_h + part * length;
             x.part = 0;
-            x.k = p.inner;
+            x.k = length;
             f32x4 acc[1] = {};
-            multiply<RAGGED, Q, __bf16, 1>(w, x, share, shares, g, acc);
+            multiply<RAGGED, true, Q, __bf16, 1>(w, x, share, shares, g, acc);
             f32x4 v;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                float sum = acc[0][c];
+            for (int i = 0; i < 4; ++i) {
+                float sum = acc[0][i];
 #pragma unroll
-                for (int o = 1; o < PH; ++o) sum += __shfl_down(acc[0][c], o);
-                v[c] = sum;
+                for (int o = 1; o < PH; ++o) sum += __shfl_down(acc[0][i], o);
+                v[i] = sum;
             }
-            if (r < PER * PH && r % PH == 0 && at < rows) *(f32x4 *)&z[share * held + base + at][g * 4] = v;
+            // lane (r, g) has the sums of rows 4 g .. 4 g + 3 of the weights with row r of h
+            if (g * 4 / COLS == part && c < PER * PH && c % PH == 0 && at < rows) *(f32x4 *)&z[(share * S + part) * held + base + at][g * 4 % COLS] = v;
         }
     }
     __syncthreads();
-    for (int o = threadIdx.x; o < p.tokens * 16; o += NT) {
-        const int t = o / 16, c = o % 16;
-        if (n0 + c >= p.width) continue;
+    for (int o = threadIdx.x; o < p.tokens * COLS; o += NT) {
+        const int t = o / COLS, col = o % COLS;
+        if (n0 + col >= p.width) continue;
         float y = 0.f;
         for (int j = 0; j < p.k; ++j) {
             const int s = t * p.k + j, row = place[s];
             if (row < 0) continue;
             float sum = 0.f;
-            for (int u = 0; u < shares; ++u) sum += z[u * held + row][c];
-            sum *= Q::scale(p.sout, (long)p.expert[s] * p.width + n0 + c);
+            for (int u = 0; u < shares * S; ++u) sum += z[u * held + row][col];
+            sum *= Q::scale(p.sout, (long)p.expert[s] * p.width + n0 + col);
             y = fmaf(p.weight ? p.weight[s] : 1.f, sum, y);
         }
-        ((T *)p.y)[t * p.ld_y + n0 + c] = narrow<T>(y);
+        ((T *)p.y)[t * p.ld_y + n0 + col] = narrow<T>(y);
     }
 }
 
@@ -433,7 +460,7 @@ int check_layer(const char *who, int64_t tokens, int k, int experts, int dtype, 
     return OPEVO_OK;
 }
 
-int64_t row_of_h(int64_t inner) { return (inner + 7) / 8 * 8; }
+int64_t row_of_h(int64_t inner) { return (inner + 2 * kStep - 1) / (2 * kStep) * (2 * kStep); }
 size_t layer_workspace(int64_t slots, int dtype, int64_t inner) { return sizeof(Plan) + (size_t)slots * (dtype == OPEVO_F32 ? 3 : 2) * row_of_h(inner) * sizeof(__bf16); }
 
 template <typename T, typename Q>
@@ -443,8 +470,15 @@ int run_layer(const Layer &p, hipStream_t stream)
     constexpr int LONG = Q::SUB * kStep;
     const bool ragged_in = p.width % LONG != 0, ragged_out = p.inner % LONG != 0;
     const int per = ragged_in ? 16 : 32;
-    if (int rc = launch("layer_in launch", ragged_in ? layer_in<T, Q, 4, true> : layer_in<T, Q, 4, false>, dim3((p.inner + per - 1) / per, groups + 1), dim3(256), stream, p)) return rc;
-    return launch("layer_out launch", ragged_out ? layer_out<T, Q, 8, true> : layer_out<T, Q, 8, false>, dim3((p.width + 15) / 16), dim3(512), stream, p);
+    if (int rc = launch("layer_in launch", ragged_in ? layer_in<T, Q, 4, true> : layer_in<T, Q, 4, false>, dim3((unsigned)((p.ld_h + per - 1) / per), groups + 1), dim3(256), stream, p)) return rc;
+    // a workgroup to 16 columns for each compute unit, or parts of K as long as that leaves units without one (us, S = 1 / 2 / 4: 1024 columns, 1 token x 2 of 4096 inner ones in 8 bits 9.3 / 7.1 /
+    // 6.4; 2048 columns, 4 x 4 of 2048 30 / 20 / 22, 64 x 8 of 1024 118 / 100 / 187; 4096 columns, 1 x 8 of 1024 12.4 / 13.2 / 19)
+    const int tiles = (p.width + 15) / 16;
+    int parts = tiles <= 80 ? 4 : tiles <= 160 ? 2 : 1;
+    while (parts > 1 && (p.inner % (parts * LONG) != 0 || 16 / parts < Parts<T>::h)) parts /= 2;
+    auto *out = ragged_out ? layer_out<T, Q, 8, 1, true> : parts == 4 ? layer_out<T, Q, 8, 4, false> : parts == 2 ? layer_out<T, Q, 8, 2, false> : layer_out<T, Q, 8, 1, false>;
+    const int cols = 16 / parts;
+    return launch("layer_out launch", out, dim3((p.width + cols - 1) / cols), dim3(512), stream, p);
 }
 template <typename T> int run_layer8(const Layer &p, hipStream_t stream) { return run_layer<T, Weights8>(p, stream); }
 template <typename T> int run_layer4(const Layer &p, hipStream_t stream) { return run_layer<T, Weights4>(p, stream); }

@@ -79,6 +79,7 @@ SIZES = [
     (1, 1, 1, 1, 1, 1.0, 0, 0), (1, 2, 8, 1024, 512, 1.0, 0, 0), (1, 2, 8, 64, 40, 0.0, 0, 0), (3, 2, 4, 17, 33, 0.7, 3, 1), (2, 3, 5, 256, 256, 1.0, 0, 0), (5, 4, 16, 320, 128, 0.9, 0, 0),
     (8, 64, 1024, 32, 24, 0.9, 0, 0), (17, 1, 3, 300, 1001, 1.0, 1, 1), (32, 4, 64, 512, 256, 1.0, 0, 0), (64, 8, 40, 256, 200, 0.8, 0, 0), (100, 5, 2, 128, 384, 1.0, 16, 0), (512, 1, 7, 96, 64, 0.9, 0, 0),
     (256, 2, 300, 130, 65, 1.0, 0, 0), (9, 1, 1, 2048, 31, 1.0, 0, 0), (1, 8, 128, 2560, 768, 1.0, 0, 0), (40, 1, 2, 33, 4096, 1.0, 0, 0), (4, 2, 1000, 1000, 77, 0.9, 5, 3),
+    (3, 2, 4, 1030, 512, 1.0, 0, 0), (20, 2, 3, 2050, 1024, 0.9, 0, 0), (1, 1, 2, 7, 2048, 1.0, 0, 0), (50, 3, 5, 1280, 1536, 1.0, 0, 0),
 ]
 
 
