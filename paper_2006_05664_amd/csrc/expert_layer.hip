@@ -24,13 +24,12 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kMaxSlots = OPEVO_EXPERT_LAYER_MAX_SLOTS;
-constexpr int kWords = OPEVO_ROUTE_MAX_EXPERTS / 32;
+constexpr int kMaxExperts = OPEVO_ROUTE_MAX_EXPERTS;
 constexpr int kStep = 128;              // values along K of four matrix instructions; lane (r, g) holds those from 32 g on of row r
 
-// What the first launch leaves for the second: the experts in use in ascending order, where each one's rows of h start (rows are the held slots, sorted by expert), and every slot's row or -1.
+// What the first launch leaves for the second: rows of h are the held slots, sorted by expert; the rows of expert e are offsets[e] .. offsets[e + 1], and row[s] is that of slot s or -1.
 struct Plan {
-    int active, held, pad[2];
-    int expert[kMaxSlots], start[kMaxSlots], row[kMaxSlots];
+    int row[kMaxSlots], offsets[kMaxExperts + 1], pad[3];
 };
 
 struct Layer {
@@ -58,6 +57,23 @@ __device__ __forceinline__ float rest(float v)
     return v == high ? 0.f : v - high;
 }
 
+// Where K ends: with an iteration, inside one, or before a row of weights has 16 bytes.
+enum Ending { kEven, kRagged, kTiny };
+
+// 16 bytes from byte `from` of a row that ends at byte `end`; what lies past it may be anything but has to be a number, as it meets activations of zero there.  A row of 16 bytes or more: its last 16,
+// shifted, for the one piece that the row ends in (by as much for all lanes), and no branch, so that all pieces are on their way together.
+template <Ending ENDING> __device__ __forceinline__ i32x4 load_end(const uint8_t *row, int from, int end)
+{
+    if (ENDING == kTiny) return load_chunk((const int8_t *)row, from, end);
+    i32x4 v, w;
+    __builtin_memcpy(&v, row + min(from, end - 16), 16);
+    const int by = (16 - end % 16) % 16;
+    w = by & 8 ? i32x4{v[2], v[3], 0, 0} : v;
+    w = by & 4 ? i32x4{w[1], w[2], w[3], 0} : w;
+    w = i32x4{(int)__builtin_amdgcn_alignbyte(w[1], w[0], by), (int)__builtin_amdgcn_alignbyte(w[2], w[1], by), (int)__builtin_amdgcn_alignbyte(w[3], w[2], by), (int)__builtin_amdgcn_alignbyte(0, w[3], by)};
+    return from > end - 16 ? w : v;
+}
+
 // ------------------------------------------------------------------ weights
 // Rows of weights, 16 of them to a tile: a lane has its row's pointer, loads 32 bytes of an iteration and makes of them the operands of SUB * 4 matrix instructions.
 struct Weights8 {
@@ -72,10 +88,10 @@ struct Weights8 {
         __builtin_memcpy(&r.v[0], row + k0 + g * 32, 16);
         __builtin_memcpy(&r.v[1], row + k0 + g * 32 + 16, 16);
     }
-    __device__ __forceinline__ void load_ragged(Raw &r, int k0, int g) const
+    template <Ending ENDING> __device__ __forceinline__ void load_last(Raw &r, int k0, int g) const
     {
-        r.v[0] = load_chunk((const int8_t *)row, k0 + g * 32, k);
-        r.v[1] = load_chunk((const int8_t *)row, k0 + g * 32 + 16, k);
+        r.v[0] = load_end<ENDING>(row, k0 + g * 32, k);
+        r.v[1] = load_end<ENDING>(row, k0 + g * 32 + 16, k);
     }
     static __device__ __forceinline__ bf16x8 operand(const Raw &r, int, int j, int)
     {
@@ -107,12 +123,13 @@ struct Weights4 {
         __builtin_memcpy(&r.v[0], row + k0 / 2 + g * 16, 16);
         __builtin_memcpy(&r.v[1], row + k0 / 2 + g * 16 + kStep / 2, 16);
     }
-    __device__ __forceinline__ void load_ragged(Raw &r, int k0, int g) const
+    template <Ending ENDING> __device__ __forceinline__ void load_last(Raw &r, int k0, int g) const
     {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            r.f[u] = load_factors(by, k0 / 32 + u * 4, (k + 31) / 32);
-            r.v[u] = load_codes(row, k0 / 2 + g * 16 + u * (kStep / 2), (k + 1) / 2, k % 2 != 0);
+            // this lane's factor, where operand() looks for it; past the last one that one again
+            r.f[u] = by[min(k0 / 32 + u * 4 + g, (k + 31) / 32 - 1)] << 8 * g;
+            r.v[u] = load_end<ENDING>(row, k0 / 2 + g * 16 + u * (kStep / 2), (k + 1) / 2);
         }
     }
     static __device__ __forceinline__ bf16x8 operand(const Raw &r, int u, int j, int g)
@@ -158,10 +175,10 @@ template <typename T> __device__ __forceinline__ bf16x8 operand(const T (&v)[8],
 
 // A lane's row of activations.  A lane without one (`on` is false) loads nothing and multiplies what its registers hold: a column of the product is its row's alone.  (Loading some row instead
 // costs as much as a row of its own: 32 tokens x 4 of 4096 x 1024, second launch, 49 us instead of 42.)
-// ORDERED: values as place_in_h puts them, rows without a ragged end.
+// ORDERED: values as place_in_h puts them, rows of whole iterations.  Else `last` is a copy of an iteration that the row ends in, filled up with zeros, in the LDS.
 template <typename T, int SUB, bool ORDERED> struct Activations {
     struct Raw { T v[SUB][4][8]; };
-    const T *row;
+    const T *row, *last;
     int part, k;
     bool on;
     __device__ __forceinline__ void load(Raw &r, int k0, int g) const
@@ -172,26 +189,20 @@ template <typename T, int SUB, bool ORDERED> struct Activations {
 #pragma unroll
             for (int j = 0; j < 4; ++j) __builtin_memcpy(r.v[u][j], row + k0 + u * kStep + (ORDERED ? j * 32 + g * 8 : g * 32 + j * 8), sizeof r.v[u][j]);
     }
-    __device__ __forceinline__ void load_ragged(Raw &r, int k0, int g) const
+    // the last iteration of a row that ends inside it, from the copy of it
+    __device__ __forceinline__ void load_last(Raw &r, int k0, int g) const
     {
         if (ORDERED) return load(r, k0, g);
-        if (!on) return;
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                constexpr int size = sizeof(T), pieces = size / 2;
-                i32x4 part[pieces];
-#pragma unroll
-                for (int o = 0; o < pieces; ++o) part[o] = load_chunk((const int8_t *)row, (k0 + u * kStep + g * 32 + j * 8) * size + o * 16, k * size);
-                __builtin_memcpy(r.v[u][j], part, sizeof part);
-            }
+            for (int j = 0; j < 4; ++j) __builtin_memcpy(r.v[u][j], __builtin_assume_aligned(last + u * kStep + g * 32 + j * 8, 16), sizeof r.v[u][j]);
     }
 };
 
 // The iterations first, first + stride, ... along K, the last one of which may be ragged; the wave whose turn it is takes that one.  The weights of the next iteration come from memory meanwhile; the
 // activations, of the same one, from the caches: they are asked for first, because loads are waited for in their order.
-template <bool RAGGED, bool ORDERED, typename Q, typename T, int NI>
+template <Ending ENDING, bool ORDERED, typename Q, typename T, int NI>
 __device__ __forceinline__ void multiply(const Q (&w)[NI], const Activations<T, Q::SUB, ORDERED> &x, int first, int stride, int g, f32x4 (&acc)[NI])
 {
     constexpr int LONG = Q::SUB * kStep;
@@ -229,204 +240,223 @@ __device__ __forceinline__ void multiply(const Q (&w)[NI], const Activations<T, 
         step(wa, wb, it);
         if (it + stride < whole) step(wb, wa, it + stride);
     }
-    if (RAGGED && whole % stride == first) {
+    if (ENDING != kEven && whole % stride == first) {
         X xr;
-        x.load_ragged(xr, whole * LONG, g);
-        __builtin_amdgcn_sched_barrier(0);
+        x.load_last(xr, whole * LONG, g);
 #pragma unroll
-        for (int n = 0; n < NI; ++n) w[n].load_ragged(wa[n], whole * LONG, g);
+        for (int n = 0; n < NI; ++n) w[n].template load_last<ENDING>(wa[n], whole * LONG, g);
         use(wa, xr);
     }
 }
 
 // ------------------------------------------------------------------ the first launch
-// The slots' experts, held ones as they are and others as -1, and a bit for every expert in use.
-template <int NT> __device__ __forceinline__ void read_slots(const Layer &p, int *ids, unsigned *words)
+// The slots' experts, held ones as they are and others as -1, and how many slots each expert has.
+template <int NT> __device__ __forceinline__ void read_slots(const Layer &p, int *ids, int *counts)
 {
-    if (threadIdx.x < kWords) words[threadIdx.x] = 0;
+    for (int e = threadIdx.x; e < p.experts; e += NT) counts[e] = 0;
     __syncthreads();
     for (int s = threadIdx.x; s < p.slots; s += NT) {
         const int e = p.expert[s];
         const bool held = (unsigned)e < (unsigned)p.experts;
         ids[s] = held ? e : -1;
-        if (held) atomicOr(&words[e >> 5], 1u << (e & 31));
+        if (held) atomicAdd(&counts[e], 1);
     }
     __syncthreads();
 }
 
-// Written by one workgroup: a slot's row is the number of held slots of lower experts, plus the earlier ones of its own.
-template <int NT> __device__ __forceinline__ void write_plan(const Layer &p, const int *ids, const unsigned *words)
+// The sums of v over the lanes up to this one.
+__device__ __forceinline__ int sum_upto(int v, int lane)
 {
-    int held = 0, active = 0;
-    for (int s = 0; s < p.slots; ++s) held += ids[s] >= 0;
-    for (int i = 0; i < kWords; ++i) active += __popc(words[i]);
-    if (threadIdx.x == 0) { p.plan->active = active; p.plan->held = held; }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(v, o);
+        if (lane >= o) v += up;
+    }
+    return v;
+}
+
+// Written by one workgroup; counts become the offsets on the way.
+template <int NT> __device__ __forceinline__ void write_plan(const Layer &p, const int *ids, int *counts, int lane)
+{
+    if (threadIdx.x < 64) {
+        int run = 0;
+        for (int e0 = 0; e0 < p.experts; e0 += 64) {
+            const int n = e0 + lane < p.experts ? counts[e0 + lane] : 0, upto = sum_upto(n, lane);
+            if (e0 + lane < p.experts) p.plan->offsets[e0 + lane] = counts[e0 + lane] = run + upto - n;
+            run += __shfl(upto, 63);
+        }
+        if (lane == 0) p.plan->offsets[p.experts] = run;
+    }
+    __syncthreads();
     for (int s = threadIdx.x; s < p.slots; s += NT) {
         const int e = ids[s];
-        int before = 0, same = 0;
-        for (int o = 0; o < p.slots; ++o) {
-            const int other = ids[o];
-            before += other >= 0 && other < e;
-            same += o < s && other == e;
-        }
-        p.plan->row[s] = e < 0 ? -1 : before + same;
-        if (e >= 0 && same == 0) {              // the first one of its expert
-            int index = __popc(words[e >> 5] & ((1u << (e & 31)) - 1u));
-            for (int i = 0; i < e >> 5; ++i) index += __popc(words[i]);
-            p.plan->expert[index] = e;
-            p.plan->start[index] = before;
-        }
+        int earlier = 0;
+        for (int o = 0; o < s; ++o) earlier += ids[o] == e;
+        p.plan->row[s] = e < 0 ? -1 : counts[e] + earlier;
     }
 }
 
-// The expert number `index` of those in use, or -1.
-__device__ __forceinline__ int expert_at(const unsigned *words, int index, int lane)
+// Every expert's rows make units of PER, the last one with fewer.  Unit number `index`: its expert, which `first`th and how many of the expert's rows, and where those start.
+struct Unit { int expert, first, rows, base; };
+template <int PER> __device__ __forceinline__ bool unit_at(const int *counts, int experts, int index, int lane, Unit *u)
 {
-    const unsigned w = lane < kWords ? words[lane] : 0;
-    const int n = __popc(w);
-    int sum = n;
-#pragma unroll
-    for (int o = 1; o < kWords; o <<= 1) {
-        const int up = __shfl_up(sum, o);
-        if (lane >= o) sum += up;
+    int seen = 0, base = 0;
+    for (int e0 = 0; e0 < experts; e0 += 64) {
+        const int n = e0 + lane < experts ? counts[e0 + lane] : 0, units = (n + PER - 1) / PER, upto = sum_upto(units, lane), rows = sum_upto(n, lane);
+        const unsigned long long past = __ballot(seen + upto > index);
+        if (past) {
+            const int at = __ffsll(past) - 1, own = __builtin_amdgcn_readlane(n, at);
+            u->expert = e0 + at;
+            u->first = (index - seen - __builtin_amdgcn_readlane(upto - units, at)) * PER;
+            u->rows = min(own - u->first, PER);
+            u->base = base + __builtin_amdgcn_readlane(rows - n, at) + u->first;
+            return true;
+        }
+        seen += __builtin_amdgcn_readlane(upto, 63);
+        base += __builtin_amdgcn_readlane(rows, 63);
     }
-    const unsigned long long past = __ballot(lane < kWords && sum > index);
-    if (!past) return -1;
-    const int at = __ffsll(past) - 1;
-    unsigned left = (unsigned)__builtin_amdgcn_readlane((int)w, at);
-    for (int skip = index - __builtin_amdgcn_readlane(sum - n, at); skip > 0; --skip) left &= left - 1;
-    return at * 32 + __ffs(left) - 1;
+    return false;
 }
 
-// h of an expert's rows for 16 * NP of its inner channels: gate and up, NP tiles of 16 rows of weights each.  The W waves deal the iterations along K among themselves.  NP is 2, so that the operands of
-// the activations serve four tiles, and 1 where K ends inside an iteration: the ragged loads would not leave registers for more.
-template <typename T, typename Q, int W, bool RAGGED>
-__global__ __launch_bounds__(W * 64, RAGGED && Parts<T>::n == 3 ? 1 : 2)
+// h of a unit's rows for 16 * NP inner channels: gate and up, NP tiles of 16 rows of weights each, so that the operands of the activations serve 2 NP tiles.  The W waves deal the iterations
+// along K among themselves.  NP is 2, or 1 where that would take more registers than there are: 4-bit weights whose rows end inside an iteration, activations in parts.
+template <typename T, typename Q, Ending ENDING> constexpr int kPairs = ENDING != kEven && Q::SUB == 2 && Parts<T>::n > 1 ? 1 : 2;
+template <typename T, typename Q, int W, Ending ENDING>
+__global__ __launch_bounds__(W * 64, 2)
 void layer_in(Layer p)
 {
-    constexpr int NT = W * 64, NP = RAGGED ? 1 : 2, NI = 2 * NP, PX = Parts<T>::n, PH = Parts<T>::h, PER = 16 / PX;
-    __shared__ int ids[kMaxSlots], list[kMaxSlots];
-    __shared__ unsigned words[kWords];
+    constexpr int NT = W * 64, NP = kPairs<T, Q, ENDING>, NI = 2 * NP, LONG = Q::SUB * kStep, PX = Parts<T>::n, PH = Parts<T>::h, PER = 16 / PX;
+    __shared__ int ids[kMaxSlots], counts[kMaxExperts], token[PER];
     __shared__ f32x4 sums[W][NI][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
-    read_slots<NT>(p, ids, words);
+    __shared__ __attribute__((aligned(16))) T last[ENDING == kEven ? 1 : PER][LONG];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15, c0 = blockIdx.x * (NP * 16);
+    read_slots<NT>(p, ids, counts);
     if (blockIdx.y == gridDim.y - 1) {
-        if (blockIdx.x == 0) write_plan<NT>(p, ids, words);
+        if (blockIdx.x == 0) write_plan<NT>(p, ids, counts, lane);
         return;
     }
-    const int e = expert_at(words, blockIdx.y, lane), c0 = blockIdx.x * (NP * 16);
-    if (e < 0) return;                      // alike for the workgroup
-    int base = 0, rows = 0;
-    for (int s0 = 0; s0 < p.slots; s0 += 64) {
-        const int id = s0 + lane < p.slots ? ids[s0 + lane] : -1;
-        const unsigned long long same = __ballot(id == e);
-        if (wave == 0 && id == e) list[rows + __popcll(same & ((1ull << lane) - 1ull))] = s0 + lane;
-        base += __popcll(__ballot(id >= 0 && id < e));
-        rows += __popcll(same);
-    }
+    Unit unit;
+    if (!unit_at<PER>(counts, p.experts, blockIdx.y, lane, &unit)) return;         // alike for the workgroup
+    if (wave == 0)
+        for (int s0 = 0, seen = -unit.first; s0 < p.slots && seen < unit.rows; s0 += 64) {
+            const bool mine = s0 + lane < p.slots && ids[s0 + lane] == unit.expert;
+            const unsigned long long same = __ballot(mine);
+            const int at = seen + __popcll(same & ((1ull << lane) - 1ull));
+            if (mine && at >= 0 && at < unit.rows) token[at] = (s0 + lane) / p.k;
+            seen += __popcll(same);
+        }
     __syncthreads();
-    const long first = (long)e * 2 * p.inner;
+    const long first = (long)unit.expert * 2 * p.inner;
     Q w[NI];
 #pragma unroll
     for (int n = 0; n < NI; ++n) w[n].at(p.win, p.ld_in, p.sin, p.ld_sin, first + (n < NP ? 0 : p.inner) + min(c0 + n % NP * 16 + r, p.inner - 1), p.width);
-    for (int t0 = 0; t0 < rows; t0 += PER) {
-        Activations<T, Q::SUB, false> x;
-        x.on = r < PER * PX && t0 + r / PX < rows;
-        x.row = (const T *)p.x + list[min(t0 + r / PX, rows - 1)] / p.k * p.ld_x;
-        x.part = r % PX;
-        x.k = p.width;
-        f32x4 acc[NI] = {};
-        multiply<RAGGED, false, Q, T, NI>(w, x, wave, W, g, acc);
-#pragma unroll
-        for (int n = 0; n < NI; ++n) sums[wave][n][lane] = acc[n];
-        __syncthreads();
-        // an output a thread: one inner channel of one row
-        for (int o = threadIdx.x; o < PER * NP * 16; o += NT) {
-            const int c = o % (NP * 16), at = o / (NP * 16), row = t0 + at;
-            if (row >= rows || c0 + c >= p.ld_h) continue;
-            __bf16 *to = p.h + (long)(base + row) * PH * p.ld_h + place_in_h(c0 + c);
-            if (c0 + c >= p.inner) {
-#pragma unroll
-                for (int part = 0; part < PH; ++part) to[part * p.ld_h] = (__bf16)0.f;
-                continue;
-            }
-            float v[2] = {0.f, 0.f};
-#pragma unroll
-            for (int side = 0; side < 2; ++side)
-#pragma unroll
-                for (int part = PX - 1; part >= 0; --part)
-                    for (int o = 0; o < W; ++o) v[side] += ((const float *)&sums[o][side * NP + c / 16][c % 16 / 4 * 16 + at * PX + part])[c % 4];
-            const float gate = v[0] * Q::scale(p.sin, first + c0 + c), up = v[1] * Q::scale(p.sin, first + p.inner + c0 + c);
-            const float h = gate / (1.f + expf(-gate)) * up, second = rest(h);
-            to[0] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(h) >> 16));
-            if constexpr (PH == 2) to[p.ld_h] = (__bf16)second;
-            else {
-                to[p.ld_h] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(second) >> 16));
-                to[2 * p.ld_h] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(rest(second)) >> 16));
-            }
+    Activations<T, Q::SUB, false> x;
+    x.on = r < unit.rows * PX;
+    x.row = (const T *)p.x + token[min(r / PX, unit.rows - 1)] * p.ld_x;
+    x.part = r % PX;
+    x.k = p.width;
+    if (ENDING != kEven) {
+        const int whole = p.width / LONG * LONG;
+        for (int i = threadIdx.x; i < unit.rows * LONG; i += NT) {
+            const int c = whole + i % LONG;
+            last[i / LONG][i % LONG] = c < p.width ? ((const T *)p.x)[token[i / LONG] * p.ld_x + c] : (T)0.f;
         }
         __syncthreads();
+        x.last = last[min(r / PX, unit.rows - 1)];
+    }
+    f32x4 acc[NI] = {};
+    multiply<ENDING, false, Q, T, NI>(w, x, wave, W, g, acc);
+#pragma unroll
+    for (int n = 0; n < NI; ++n) sums[wave][n][lane] = acc[n];
+    __syncthreads();
+    // an output a thread: one inner channel of one row
+    for (int o = threadIdx.x; o < unit.rows * NP * 16; o += NT) {
+        const int c = o % (NP * 16), at = o / (NP * 16);
+        if (c0 + c >= p.ld_h) continue;
+        __bf16 *to = p.h + (long)(unit.base + at) * PH * p.ld_h + place_in_h(c0 + c);
+        if (c0 + c >= p.inner) {
+#pragma unroll
+            for (int part = 0; part < PH; ++part) to[part * p.ld_h] = (__bf16)0.f;
+            continue;
+        }
+        float v[2] = {0.f, 0.f};
+#pragma unroll
+        for (int side = 0; side < 2; ++side)
+#pragma unroll
+            for (int part = PX - 1; part >= 0; --part)
+                for (int o = 0; o < W; ++o) v[side] += ((const float *)&sums[o][side * NP + c / 16][c % 16 / 4 * 16 + at * PX + part])[c % 4];
+        const float gate = v[0] * Q::scale(p.sin, first + c0 + c), up = v[1] * Q::scale(p.sin, first + p.inner + c0 + c);
+        const float h = gate / (1.f + expf(-gate)) * up, second = rest(h);
+        to[0] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(h) >> 16));
+        if constexpr (PH == 2) to[p.ld_h] = (__bf16)second;
+        else {
+            to[p.ld_h] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(second) >> 16));
+            to[2 * p.ld_h] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(rest(second)) >> 16));
+        }
     }
 }
 
 // ------------------------------------------------------------------ the second launch
-// y of COLS = 16 / S columns for all tokens: a task is an expert in use and a share of K, the W waves deal the tasks among themselves, what they find for each row meets in LDS, and the rows of
+// y of COLS = 16 / S columns for all tokens: a task is a unit of rows of an expert and a share of K, the W waves deal the tasks among themselves, what they find for each row meets in LDS, and the rows of
 // a token are added up there in the order of its slots.
 // S > 1, for few tokens and few columns: K falls into S parts, and the 16 rows of weights of a product are COLS columns in each of the parts, the 16 rows of h COLS rows in each of
 // them.  Of the product the S blocks of a part with itself are used; a wave reads as much as ever, and there are S times as many workgroups.
 constexpr int kShares = 1024;           // rows of 16 sums in the LDS
 
-template <typename T, typename Q, int W, int S, bool RAGGED>
+template <typename T, typename Q, int W, int S, Ending ENDING>
 __global__ __launch_bounds__(W * 64)
 void layer_out(Layer p)
 {
     constexpr int NT = W * 64, COLS = 16 / S, PH = Parts<T>::h, PER = COLS / PH;
-    static_assert(PER >= 1 && (S == 1 || !RAGGED), "");
-    __shared__ int expert[kMaxSlots], start[kMaxSlots], place[kMaxSlots];
+    static_assert(PER >= 1 && (S == 1 || ENDING == kEven), "");
+    __shared__ int place[kMaxSlots], total;
+    __shared__ Unit units[kMaxSlots];
     __shared__ __attribute__((aligned(16))) float z[kShares * S][COLS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15, part = r / COLS, c = r % COLS, n0 = blockIdx.x * COLS;
-    for (int s = threadIdx.x; s < p.slots; s += NT) {
-        expert[s] = p.plan->expert[s];
-        start[s] = p.plan->start[s];
-        place[s] = p.plan->row[s];
+    const int held = __builtin_amdgcn_readfirstlane(p.plan->offsets[p.experts]);
+    for (int s = threadIdx.x; s < p.slots; s += NT) place[s] = p.plan->row[s];
+    if (wave == 0) {
+        int seen = 0;
+        for (int e0 = 0; e0 < p.experts; e0 += 64) {
+            const int e = e0 + lane, lo = e < p.experts ? p.plan->offsets[e] : 0, rows = e < p.experts ? p.plan->offsets[e + 1] - lo : 0, n = (rows + PER - 1) / PER, upto = sum_upto(n, lane);
+            for (int i = 0; i < n; ++i) units[seen + upto - n + i] = {e, i * PER, min(rows - i * PER, PER), lo + i * PER};
+            seen += __shfl(upto, 63);
+        }
+        if (lane == 0) total = seen;
     }
-    const int active = __builtin_amdgcn_readfirstlane(p.plan->active), held = __builtin_amdgcn_readfirstlane(p.plan->held);
     __syncthreads();
-    const int length = p.inner / S, count = (length + Q::SUB * kStep - 1) / (Q::SUB * kStep);
+    const int length = p.inner / S, count = (length + Q::SUB * kStep - 1) / (Q::SUB * kStep), all = __builtin_amdgcn_readfirstlane(total);
     // shares of K: as many as make the waves' iterations fewest, two lost to each task's start
     int shares = 1, least = INT32_MAX;
     for (int s = 1; s <= W && s <= count && s * held <= kShares; s *= 2) {
-        const int cost = (active * s + W - 1) / W * ((count + s - 1) / s + 2);
+        const int cost = (all * s + W - 1) / W * ((count + s - 1) / s + 2);
         if (cost < least) { least = cost; shares = s; }
     }
     const int shift = __builtin_ctz(shares);
-    for (int task = wave; task < active * shares; task += W) {
-        const int index = task >> shift, share = task & (shares - 1);
-        const int e = __builtin_amdgcn_readfirstlane(expert[index]), base = __builtin_amdgcn_readfirstlane(start[index]),
-                  rows = (index + 1 < active ? __builtin_amdgcn_readfirstlane(start[index + 1]) : held) - base;
+    for (int task = wave; task < all * shares; task += W) {
+        const int share = task & (shares - 1);
+        const Unit unit = units[task >> shift];
+        const int e = __builtin_amdgcn_readfirstlane(unit.expert), base = __builtin_amdgcn_readfirstlane(unit.base), rows = __builtin_amdgcn_readfirstlane(unit.rows), at = c / PH;
         Q w[1];
         w[0].at(p.wout, p.ld_out, p.sout, p.ld_sout, (long)e * p.width + min(n0 + c, p.width - 1), p.inner);
         if (S > 1) w[0].skip(part * length);
-        for (int t0 = 0; t0 < rows; t0 += PER) {
-            const int at = t0 + c / PH;
-            Activations<__bf16, Q::SUB, true> x;
-            x.on = c < PER * PH && at < rows;
-            x.row = p.h + ((long)(base + min(at, rows - 1)) * PH + c % PH) * p.ld_h + part * length;
-            x.part = 0;
-            x.k = length;
-            f32x4 acc[1] = {};
-            multiply<RAGGED, true, Q, __bf16, 1>(w, x, share, shares, g, acc);
-            f32x4 v;
+        Activations<__bf16, Q::SUB, true> x;
+        x.on = c < rows * PH;
+        x.row = p.h + ((long)(base + min(at, rows - 1)) * PH + c % PH) * p.ld_h + part * length;
+        x.part = 0;
+        x.k = length;
+        f32x4 acc[1] = {};
+        multiply<ENDING, true, Q, __bf16, 1>(w, x, share, shares, g, acc);
+        f32x4 v;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float sum = acc[0][i];
+        for (int i = 0; i < 4; ++i) {
+            float sum = acc[0][i];
 #pragma unroll
-                for (int o = 1; o < PH; ++o) sum += __shfl_down(acc[0][i], o);
-                v[i] = sum;
-            }
-            // lane (r, g) has the sums of rows 4 g .. 4 g + 3 of the weights with row r of h
-            if (g * 4 / COLS == part && c < PER * PH && c % PH == 0 && at < rows) *(f32x4 *)&z[(share * S + part) * held + base + at][g * 4 % COLS] = v;
+            for (int o = 1; o < PH; ++o) sum += __shfl_down(acc[0][i], o);
+            v[i] = sum;
         }
+        // lane (r, g) has the sums of rows 4 g .. 4 g + 3 of the weights with row r of h
+        if (g * 4 / COLS == part && c < rows * PH && c % PH == 0) *(f32x4 *)&z[(share * S + part) * held + base + at][g * 4 % COLS] = v;
     }
     __syncthreads();
     for (int o = threadIdx.x; o < p.tokens * COLS; o += NT) {
@@ -466,17 +496,21 @@ size_t layer_workspace(int64_t slots, int dtype, int64_t inner) { return sizeof(
 template <typename T, typename Q>
 int run_layer(const Layer &p, hipStream_t stream)
 {
-    const int groups = std::min(p.slots, p.experts);
+    constexpr int PER = 16 / Parts<T>::n;
+    const int units = std::min(p.slots, std::min(p.slots, p.experts) + p.slots / PER);      // there can be no more
     constexpr int LONG = Q::SUB * kStep;
-    const bool ragged_in = p.width % LONG != 0, ragged_out = p.inner % LONG != 0;
-    const int per = ragged_in ? 16 : 32;
-    if (int rc = launch("layer_in launch", ragged_in ? layer_in<T, Q, 4, true> : layer_in<T, Q, 4, false>, dim3((unsigned)((p.ld_h + per - 1) / per), groups + 1), dim3(256), stream, p)) return rc;
+    const auto ending = [](int k) { return k % LONG == 0 ? kEven : k * Q::SUB == k ? (k < 16 ? kTiny : kRagged) : k < 31 ? kTiny : kRagged; };       // a byte a value, or half a byte
+    const Ending in = ending(p.width), of = ending(p.inner);
+    auto *first = in == kEven ? layer_in<T, Q, 4, kEven> : in == kRagged ? layer_in<T, Q, 4, kRagged> : layer_in<T, Q, 4, kTiny>;
+    const int channels = 16 * (in == kEven ? kPairs<T, Q, kEven> : kPairs<T, Q, kRagged>);
+    if (int rc = launch("layer_in launch", first, dim3((unsigned)(p.ld_h / channels), units + 1), dim3(256), stream, p)) return rc;
     // a workgroup to 16 columns for each compute unit, or parts of K as long as that leaves units without one (us, S = 1 / 2 / 4: 1024 columns, 1 token x 2 of 4096 inner ones in 8 bits 9.3 / 7.1 /
     // 6.4; 2048 columns, 4 x 4 of 2048 30 / 20 / 22, 64 x 8 of 1024 118 / 100 / 187; 4096 columns, 1 x 8 of 1024 12.4 / 13.2 / 19)
     const int tiles = (p.width + 15) / 16;
     int parts = tiles <= 80 ? 4 : tiles <= 160 ? 2 : 1;
     while (parts > 1 && (p.inner % (parts * LONG) != 0 || 16 / parts < Parts<T>::h)) parts /= 2;
-    auto *out = ragged_out ? layer_out<T, Q, 8, 1, true> : parts == 4 ? layer_out<T, Q, 8, 4, false> : parts == 2 ? layer_out<T, Q, 8, 2, false> : layer_out<T, Q, 8, 1, false>;
+    auto *out = of == kTiny ? layer_out<T, Q, 8, 1, kTiny> : of == kRagged ? layer_out<T, Q, 8, 1, kRagged>
+                : parts == 4 ? layer_out<T, Q, 8, 4, kEven> : parts == 2 ? layer_out<T, Q, 8, 2, kEven> : layer_out<T, Q, 8, 1, kEven>;
     const int cols = 16 / parts;
     return launch("layer_out launch", out, dim3((p.width + cols - 1) / cols), dim3(512), stream, p);
 }
