@@ -27,9 +27,14 @@ constexpr int kMaxSlots = OPEVO_EXPERT_LAYER_MAX_SLOTS;
 constexpr int kMaxExperts = OPEVO_ROUTE_MAX_EXPERTS;
 constexpr int kStep = 128;              // values along K of four matrix instructions; lane (r, g) holds those from 32 g on of row r
 
-// What the first launch leaves for the second: rows of h are the held slots, sorted by expert; the rows of expert e are offsets[e] .. offsets[e + 1], and row[s] is that of slot s or -1.
+// Some rows of one expert: `rows` of them from row `base` of h on, the `first`th and later ones of a group of tokens.
+struct Unit { int expert, first, rows, base; };
+
+// What the first launch leaves for the second, for every group of tokens (a group's slots are a stretch, and it has no more units than slots, which start where its slots do): its units and rows, and the
+// place of each slot's row among the group's, or -1.
 struct Plan {
-    int row[kMaxSlots], offsets[kMaxExperts + 1], pad[3];
+    int units_of[kMaxSlots], rows_of[kMaxSlots], place[kMaxSlots];
+    Unit units[kMaxSlots];
 };
 
 struct Layer {
@@ -44,6 +49,7 @@ struct Layer {
     void *y;
     long ld_y;
     Plan *plan;
+    int groups, group_tokens, group_unit;       // of the second launch: groups of tokens, how many tokens and how many rows of a unit
     __bf16 *h;                          // [held slots][parts][ld_h], zeros from `inner` on
     long ld_h;
 };
@@ -275,29 +281,54 @@ __device__ __forceinline__ int sum_upto(int v, int lane)
     return v;
 }
 
-// Written by one workgroup; counts become the offsets on the way.
-template <int NT> __device__ __forceinline__ void write_plan(const Layer &p, const int *ids, int *counts, int lane)
+// Exclusive sums of counts over the experts, by one wave, in place.
+__device__ __forceinline__ void add_up(int *counts, int experts, int lane)
 {
-    if (threadIdx.x < 64) {
-        int run = 0;
-        for (int e0 = 0; e0 < p.experts; e0 += 64) {
-            const int n = e0 + lane < p.experts ? counts[e0 + lane] : 0, upto = sum_upto(n, lane);
-            if (e0 + lane < p.experts) p.plan->offsets[e0 + lane] = counts[e0 + lane] = run + upto - n;
-            run += __shfl(upto, 63);
-        }
-        if (lane == 0) p.plan->offsets[p.experts] = run;
-    }
-    __syncthreads();
-    for (int s = threadIdx.x; s < p.slots; s += NT) {
-        const int e = ids[s];
-        int earlier = 0;
-        for (int o = 0; o < s; ++o) earlier += ids[o] == e;
-        p.plan->row[s] = e < 0 ? -1 : counts[e] + earlier;
+    int run = 0;
+    for (int e0 = 0; e0 < experts; e0 += 64) {
+        const int n = e0 + lane < experts ? counts[e0 + lane] : 0, upto = sum_upto(n, lane);
+        if (e0 + lane < experts) counts[e0 + lane] = run + upto - n;
+        run += __builtin_amdgcn_readlane(upto, 63);
     }
 }
 
-// Every expert's rows make units of PER, the last one with fewer.  Unit number `index`: its expert, which `first`th and how many of the expert's rows, and where those start.
-struct Unit { int expert, first, rows, base; };
+// The plan of one group of tokens, by one workgroup.  before: the slots of lower experts (rows of h are the held slots, sorted by expert); earlier, own: an expert's slots in front of the group
+// and in it.
+template <int NT> __device__ __forceinline__ void write_plan(const Layer &p, const int *ids, const int *before, int *earlier, int *own, int group, int lane)
+{
+    const int first = group * p.group_tokens * p.k, last = min(first + p.group_tokens * p.k, p.slots);
+    __syncthreads();
+    for (int e = threadIdx.x; e < p.experts; e += NT) earlier[e] = own[e] = 0;
+    __syncthreads();
+    for (int s = threadIdx.x; s < last; s += NT)
+        if (ids[s] >= 0) atomicAdd(s < first ? &earlier[ids[s]] : &own[ids[s]], 1);
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        int units = 0, rows = 0;
+        for (int e0 = 0; e0 < p.experts; e0 += 64) {
+            const int e = e0 + lane, mine = e < p.experts ? own[e] : 0, n = (mine + p.group_unit - 1) / p.group_unit, upto = sum_upto(n, lane), rows_upto = sum_upto(mine, lane);
+            const int at = rows + rows_upto - mine;
+            for (int i = 0; i < n; ++i)
+                p.plan->units[first + units + upto - n + i] = {e, at + i * p.group_unit, min(mine - i * p.group_unit, p.group_unit), before[e] + earlier[e] + i * p.group_unit};
+            if (e < p.experts) own[e] = at;
+            units += __builtin_amdgcn_readlane(upto, 63);
+            rows += __builtin_amdgcn_readlane(rows_upto, 63);
+        }
+        if (lane == 0) {
+            p.plan->units_of[group] = units;
+            p.plan->rows_of[group] = rows;
+        }
+    }
+    __syncthreads();
+    for (int s = first + threadIdx.x; s < last; s += NT) {
+        const int e = ids[s];
+        int rank = 0;
+        for (int o = first; o < s; ++o) rank += ids[o] == e;
+        p.plan->place[s] = e < 0 ? -1 : own[e] + rank;
+    }
+}
+
+// Every expert's rows make units of PER, the last one with fewer.  Unit number `index` of all; `first` counts the expert's rows.
 template <int PER> __device__ __forceinline__ bool unit_at(const int *counts, int experts, int index, int lane, Unit *u)
 {
     int seen = 0, base = 0;
@@ -332,7 +363,10 @@ void layer_in(Layer p)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15, c0 = blockIdx.x * (NP * 16);
     read_slots<NT>(p, ids, counts);
     if (blockIdx.y == gridDim.y - 1) {
-        if (blockIdx.x == 0) write_plan<NT>(p, ids, counts, lane);
+        if (threadIdx.x < 64) add_up(counts, p.experts, lane);
+        int *const more = (int *)sums;
+        static_assert(sizeof sums >= 2 * kMaxExperts * sizeof(int), "");
+        for (int group = blockIdx.x; group < p.groups; group += gridDim.x) write_plan<NT>(p, ids, counts, more, more + kMaxExperts, group, lane);
         return;
     }
     Unit unit;
@@ -397,9 +431,10 @@ void layer_in(Layer p)
 }
 
 // ------------------------------------------------------------------ the second launch
-// y of COLS = 16 / S columns for all tokens: a task is a unit of rows of an expert and a share of K, the W waves deal the tasks among themselves, what they find for each row meets in LDS, and the rows of
-// a token are added up there in the order of its slots.
-// S > 1, for few tokens and few columns: K falls into S parts, and the 16 rows of weights of a product are COLS columns in each of the parts, the 16 rows of h COLS rows in each of
+// y of COLS = 16 / S columns for a group of tokens: a task is a unit of rows of an expert and a share of K, the W waves deal the tasks among themselves, what they find for each row
+// meets in LDS, and the rows of a token are added up there in the order of its slots.  A wave goes through its tasks' iterations as one sequence, the next two on their way from memory whichever task
+// they belong to: an iteration is a few microseconds' worth of latency and a fraction of one of work.
+// S > 1, for few columns: K falls into S parts, and the 16 rows of weights of a product are COLS columns in each of the parts, the 16 rows of h COLS rows in each of
 // them.  Of the product the S blocks of a part with itself are used; a wave reads as much as ever, and there are S times as many workgroups.
 constexpr int kShares = 1024;           // rows of 16 sums in the LDS
 
@@ -407,71 +442,107 @@ template <typename T, typename Q, int W, int S, Ending ENDING>
 __global__ __launch_bounds__(W * 64)
 void layer_out(Layer p)
 {
-    constexpr int NT = W * 64, COLS = 16 / S, PH = Parts<T>::h, PER = COLS / PH;
+    constexpr int NT = W * 64, COLS = 16 / S, PH = Parts<T>::h, PER = COLS / PH, LONG = Q::SUB * kStep;
     static_assert(PER >= 1 && (S == 1 || ENDING == kEven), "");
-    __shared__ int place[kMaxSlots], total;
+    __shared__ int place[kMaxSlots];
     __shared__ Unit units[kMaxSlots];
     __shared__ __attribute__((aligned(16))) float z[kShares * S][COLS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15, part = r / COLS, c = r % COLS, n0 = blockIdx.x * COLS;
-    const int held = __builtin_amdgcn_readfirstlane(p.plan->offsets[p.experts]);
-    for (int s = threadIdx.x; s < p.slots; s += NT) place[s] = p.plan->row[s];
-    if (wave == 0) {
-        int seen = 0;
-        for (int e0 = 0; e0 < p.experts; e0 += 64) {
-            const int e = e0 + lane, lo = e < p.experts ? p.plan->offsets[e] : 0, rows = e < p.experts ? p.plan->offsets[e + 1] - lo : 0, n = (rows + PER - 1) / PER, upto = sum_upto(n, lane);
-            for (int i = 0; i < n; ++i) units[seen + upto - n + i] = {e, i * PER, min(rows - i * PER, PER), lo + i * PER};
-            seen += __shfl(upto, 63);
-        }
-        if (lane == 0) total = seen;
+    const int t0 = blockIdx.y * p.group_tokens, tokens = min(p.group_tokens, p.tokens - t0), first = t0 * p.k;
+    const int all = __builtin_amdgcn_readfirstlane(p.plan->units_of[blockIdx.y]), here = __builtin_amdgcn_readfirstlane(p.plan->rows_of[blockIdx.y]);
+    for (int s = threadIdx.x; s < tokens * p.k; s += NT) {
+        place[s] = p.plan->place[first + s];
+        units[s] = p.plan->units[first + s];
     }
     __syncthreads();
-    const int length = p.inner / S, count = (length + Q::SUB * kStep - 1) / (Q::SUB * kStep), all = __builtin_amdgcn_readfirstlane(total);
-    // shares of K: as many as make the waves' iterations fewest, two lost to each task's start
+    const int length = p.inner / S, whole = length / LONG, count = (length + LONG - 1) / LONG;
+    // shares of K: as many as make the waves' iterations fewest, one lost to each task
     int shares = 1, least = INT32_MAX;
-    for (int s = 1; s <= W && s <= count && s * held <= kShares; s *= 2) {
-        const int cost = (all * s + W - 1) / W * ((count + s - 1) / s + 2);
+    for (int s = 1; s <= W && s <= count && s * here <= kShares; s *= 2) {
+        const int cost = (all * s + W - 1) / W * ((count + s - 1) / s + 1);
         if (cost < least) { least = cost; shares = s; }
     }
-    const int shift = __builtin_ctz(shares);
-    for (int task = wave; task < all * shares; task += W) {
-        const int share = task & (shares - 1);
+    const int shift = __builtin_ctz(shares), tasks = all * shares;
+
+    // The sequence of this wave's iterations, as it is loaded and as it is used.
+    struct Place { int task, it; };
+    auto begin = [&](int task) { return Place{task, task & (shares - 1)}; };
+    Place load_at = begin(wave), use_at = load_at;
+    Q w;
+    Activations<__bf16, Q::SUB, true> x;
+    x.part = 0;
+    x.k = length;
+    x.last = nullptr;
+    auto aim = [&](int task) {
         const Unit unit = units[task >> shift];
-        const int e = __builtin_amdgcn_readfirstlane(unit.expert), base = __builtin_amdgcn_readfirstlane(unit.base), rows = __builtin_amdgcn_readfirstlane(unit.rows), at = c / PH;
-        Q w[1];
-        w[0].at(p.wout, p.ld_out, p.sout, p.ld_sout, (long)e * p.width + min(n0 + c, p.width - 1), p.inner);
-        if (S > 1) w[0].skip(part * length);
-        Activations<__bf16, Q::SUB, true> x;
+        const int e = __builtin_amdgcn_readfirstlane(unit.expert), base = __builtin_amdgcn_readfirstlane(unit.base), rows = __builtin_amdgcn_readfirstlane(unit.rows);
+        w.at(p.wout, p.ld_out, p.sout, p.ld_sout, (long)e * p.width + min(n0 + c, p.width - 1), p.inner);
+        if (S > 1) w.skip(part * length);
         x.on = c < rows * PH;
-        x.row = p.h + ((long)(base + min(at, rows - 1)) * PH + c % PH) * p.ld_h + part * length;
-        x.part = 0;
-        x.k = length;
-        f32x4 acc[1] = {};
-        multiply<ENDING, true, Q, __bf16, 1>(w, x, share, shares, g, acc);
+        x.row = p.h + ((long)(base + min(c / PH, rows - 1)) * PH + c % PH) * p.ld_h + part * length;
+    };
+    struct Buffer { typename Q::Raw w; typename Activations<__bf16, Q::SUB, true>::Raw x; } b0, b1, b2;
+    auto load = [&](Buffer &b) {
+        if (load_at.task >= tasks) return;
+        x.load(b.x, load_at.it * LONG, g);
+        if (ENDING == kEven || load_at.it < whole) w.load(b.w, load_at.it * LONG, g);
+        else w.template load_last<ENDING>(b.w, load_at.it * LONG, g);
+        load_at.it += shares;
+        if (load_at.it >= count) {
+            load_at = begin(load_at.task + W);
+            if (load_at.task < tasks) aim(load_at.task);
+        }
+    };
+    f32x4 acc = {};
+    auto use = [&](const Buffer &b) {
+#pragma unroll
+        for (int u = 0; u < Q::SUB; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Q::operand(b.w, u, j, g), operand(b.x.v[u][j], 0), acc, 0, 0, 0);
+        asm volatile("" : "+v"(acc));           // due here, not behind the next branch
+        use_at.it += shares;
+        if (use_at.it < count) return;
+        const Unit unit = units[use_at.task >> shift];
         f32x4 v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float sum = acc[0][i];
+            float sum = acc[i];
 #pragma unroll
-            for (int o = 1; o < PH; ++o) sum += __shfl_down(acc[0][i], o);
+            for (int o = 1; o < PH; ++o) sum += __shfl_down(acc[i], o);
             v[i] = sum;
         }
         // lane (r, g) has the sums of rows 4 g .. 4 g + 3 of the weights with row r of h
-        if (g * 4 / COLS == part && c < rows * PH && c % PH == 0) *(f32x4 *)&z[(share * S + part) * held + base + at][g * 4 % COLS] = v;
+        if (g * 4 / COLS == part && c < unit.rows * PH && c % PH == 0) *(f32x4 *)&z[((use_at.task & (shares - 1)) * S + part) * here + unit.first + c / PH][g * 4 % COLS] = v;
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
+        use_at = begin(use_at.task + W);
+    };
+    if (load_at.task < tasks) aim(load_at.task);
+    load(b0);
+    load(b1);
+    while (use_at.task < tasks) {
+        load(b2);
+        use(b0);
+        if (use_at.task >= tasks) break;
+        load(b0);
+        use(b1);
+        if (use_at.task >= tasks) break;
+        load(b1);
+        use(b2);
     }
     __syncthreads();
-    for (int o = threadIdx.x; o < p.tokens * COLS; o += NT) {
+    for (int o = threadIdx.x; o < tokens * COLS; o += NT) {
         const int t = o / COLS, col = o % COLS;
         if (n0 + col >= p.width) continue;
         float y = 0.f;
         for (int j = 0; j < p.k; ++j) {
-            const int s = t * p.k + j, row = place[s];
+            const int row = place[t * p.k + j], s = first + t * p.k + j;
             if (row < 0) continue;
             float sum = 0.f;
-            for (int u = 0; u < shares * S; ++u) sum += z[u * held + row][col];
+            for (int u = 0; u < shares * S; ++u) sum += z[u * here + row][col];
             sum *= Q::scale(p.sout, (long)p.expert[s] * p.width + n0 + col);
             y = fmaf(p.weight ? p.weight[s] : 1.f, sum, y);
         }
-        ((T *)p.y)[t * p.ld_y + n0 + col] = narrow<T>(y);
+        ((T *)p.y)[(t0 + t) * p.ld_y + n0 + col] = narrow<T>(y);
     }
 }
 
@@ -494,25 +565,31 @@ int64_t row_of_h(int64_t inner) { return (inner + 2 * kStep - 1) / (2 * kStep) *
 size_t layer_workspace(int64_t slots, int dtype, int64_t inner) { return sizeof(Plan) + (size_t)slots * (dtype == OPEVO_F32 ? 3 : 2) * row_of_h(inner) * sizeof(__bf16); }
 
 template <typename T, typename Q>
-int run_layer(const Layer &p, hipStream_t stream)
+int run_layer(Layer p, hipStream_t stream)
 {
-    constexpr int PER = 16 / Parts<T>::n;
-    const int units = std::min(p.slots, std::min(p.slots, p.experts) + p.slots / PER);      // there can be no more
-    constexpr int LONG = Q::SUB * kStep;
-    const auto ending = [](int k) { return k % LONG == 0 ? kEven : k * Q::SUB == k ? (k < 16 ? kTiny : kRagged) : k < 31 ? kTiny : kRagged; };       // a byte a value, or half a byte
+    constexpr int LONG = Q::SUB * kStep, PER = 16 / Parts<T>::n;
+    const auto ending = [](int k) { return k % LONG == 0 ? kEven : k < (Q::SUB == 1 ? 16 : 31) ? kTiny : kRagged; };
     const Ending in = ending(p.width), of = ending(p.inner);
-    auto *first = in == kEven ? layer_in<T, Q, 4, kEven> : in == kRagged ? layer_in<T, Q, 4, kRagged> : layer_in<T, Q, 4, kTiny>;
-    const int channels = 16 * (in == kEven ? kPairs<T, Q, kEven> : kPairs<T, Q, kRagged>);
-    if (int rc = launch("layer_in launch", first, dim3((unsigned)(p.ld_h / channels), units + 1), dim3(256), stream, p)) return rc;
-    // a workgroup to 16 columns for each compute unit, or parts of K as long as that leaves units without one (us, S = 1 / 2 / 4: 1024 columns, 1 token x 2 of 4096 inner ones in 8 bits 9.3 / 7.1 /
-    // 6.4; 2048 columns, 4 x 4 of 2048 30 / 20 / 22, 64 x 8 of 1024 118 / 100 / 187; 4096 columns, 1 x 8 of 1024 12.4 / 13.2 / 19)
+    // The second launch: a workgroup to 16 columns for each compute unit, or parts of K as long as that leaves units without one (us, S = 1 / 2 / 4: 1024 columns, 1 token x 2 of 4096 inner ones in
+    // 8 bits 9.3 / 7.1 / 6.4; 2048 columns, 4 x 4 of 2048 30 / 20 / 22, 64 x 8 of 1024 118 / 100 / 187; 4096 columns, 1 x 8 of 1024 12.4 / 13.2 / 19) ...
     const int tiles = (p.width + 15) / 16;
     int parts = tiles <= 80 ? 4 : tiles <= 160 ? 2 : 1;
     while (parts > 1 && (p.inner % (parts * LONG) != 0 || 16 / parts < Parts<T>::h)) parts /= 2;
     auto *out = of == kTiny ? layer_out<T, Q, 8, 1, kTiny> : of == kRagged ? layer_out<T, Q, 8, 1, kRagged>
                 : parts == 4 ? layer_out<T, Q, 8, 4, kEven> : parts == 2 ? layer_out<T, Q, 8, 2, kEven> : layer_out<T, Q, 8, 1, kEven>;
-    const int cols = 16 / parts;
-    return launch("layer_out launch", out, dim3((p.width + cols - 1) / cols), dim3(512), stream, p);
+    // ... and where that is not enough the tokens in groups, each of which reads its experts' weights again, mostly from the caches (us, one sequence of iterations and groups against neither: 4-bit
+    // weights, 102 tokens x 2 of 8 experts, 246 columns of 2879 inner ones, fp16 61 / 132; 126 x 1 of 15, 469 of 1280, fp32 47 / 81; 8 bits, 32 x 1 of 62, 64 of 525 10 / 19)
+    const int cols = 16 / parts, across = (p.width + cols - 1) / cols;
+    p.groups = std::min(p.tokens, std::max(1, 256 / across));
+    p.group_tokens = (p.tokens + p.groups - 1) / p.groups;
+    p.groups = (p.tokens + p.group_tokens - 1) / p.group_tokens;
+    p.group_unit = cols / Parts<T>::h;
+
+    const int units = std::min(p.slots, std::min(p.slots, p.experts) + p.slots / PER);      // of the first launch; there can be no more
+    const int channels = 16 * (in == kEven ? kPairs<T, Q, kEven> : kPairs<T, Q, kRagged>);
+    auto *first = in == kEven ? layer_in<T, Q, 4, kEven> : in == kRagged ? layer_in<T, Q, 4, kRagged> : layer_in<T, Q, 4, kTiny>;
+    if (int rc = launch("layer_in launch", first, dim3((unsigned)(p.ld_h / channels), units + 1), dim3(256), stream, p)) return rc;
+    return launch("layer_out launch", out, dim3(across, p.groups), dim3(512), stream, p);
 }
 template <typename T> int run_layer8(const Layer &p, hipStream_t stream) { return run_layer<T, Weights8>(p, stream); }
 template <typename T> int run_layer4(const Layer &p, hipStream_t stream) { return run_layer<T, Weights4>(p, stream); }
