@@ -26,6 +26,7 @@ OPEVO_FACTOR, OPEVO_PERMUTATION, OPEVO_DISCRETE, OPEVO_CATEGORICAL = 0, 1, 2, 3
 OPEVO_MATMUL, OPEVO_BMM, OPEVO_CONV2D, OPEVO_BMM_TA = 0, 1, 2, 3
 OPEVO_F32, OPEVO_BF16, OPEVO_F16 = 0, 1, 2
 OPEVO_ROUTE_MAX_EXPERTS, OPEVO_ROUTE_MAX_SLOTS = 1024, 64
+OPEVO_EXPERT_LAYER_MAX_SLOTS = 512
 OPEVO_TILE2, OPEVO_TILE4, OPEVO_TILE4X, OPEVO_TILE4P, OPEVO_TILE4K, OPEVO_TILE4C, OPEVO_TILE4T, OPEVO_TILE4A, OPEVO_TILE4L = 0, 1, 2, 3, 4, 5, 6, 7, 8
 
 
