@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <type_traits>
 
@@ -74,7 +75,7 @@ __device__ __forceinline__ void store_sums(const Product4 &p, const Rows &r, int
             if (row0 + row >= r.last || c >= cols) continue;
             T *dst = (T *)p.c + (row0 + row) * p.ldc + col0 + c;
             const int8_t *from = patch + row * PITCH + (at % CPR ^ row % CPR) * 16;
-            if (c + V <= cols) __builtin_memcpy(dst, __builtin_assume_aligned(from, 16), 16);
+            if (c + V <= cols) store_away(dst, __builtin_assume_aligned(from, 16));       // 8192 x 4096 x 1024 bf16 31.9 -> 29.3 us, 2048 rows 9.8 -> 8.0; as much less with a reader
             else
 #pragma unroll 1
                 for (int e = 0; e < cols - c; ++e) dst[e] = ((const T *)from)[e];
@@ -648,7 +649,7 @@ int run_thin(const Product4 &p, hipStream_t stream)
 // A kernel and what it takes, in us: launch + max(steps * chain, load * (tile + steps * rate)), where steps is how many slabs (thin: steps of 256 bytes) a wave
 // goes through and load the workgroups for each of the 256 compute units, rounded up where that foretold the times better.  The first term is a workgroup's chain of latencies,
 // the second what a compute unit gets through.  The constants were fitted to the times of every kernel at 750 random sizes of 1 - 8192 rows, 64 - 8192 columns and K of 64 - 8192 (a third
-// each of K in multiples of 1024, of 32, and any), those near the best one's counting most; the kernel chosen by them took 1.5, 3.5 and 1.7 % more than the best of all
+// each of K in multiples of 1024, of 32, and any), those near the best one's counting most; the kernel chosen by them took 2.3, 2.8 and 1.8 % more than the best of all
 // in the geometric mean, at most 1.9 times as much.  By experts they are used with the tiles that an even deal of the rows would make.
 struct Kernel {
     int (*run)(const Product4 &, hipStream_t);
@@ -659,27 +660,27 @@ struct Kernel {
 };
 constexpr int64_t kAll = INT64_MAX;
 const Kernel kLong[] = {                // besides those of kDirect
-    {run_long<LongShape<256, 256, 2, 4, 2>>, 256, 256, 128, 1, kAll, false, 6.81f, 1.43f, 5.13f, 2.32f},
-    {run_long<LongShape<128, 128, 2, 2, 2>>, 128, 128, 128, 1, kAll, false, 4.12f, 0.561f, 1.83f, 0.686f},
-    {run_long<LongShape<128, 128, 2, 4, 4>>, 128, 128, 128, 1, kAll, false, 3.59f, 0.546f, 2.08f, 0.889f},
+    {run_long<LongShape<256, 256, 2, 4, 2>>, 256, 256, 128, 1, kAll, false, 6.78f, 1.38f, 8.53f, 2.33f},
+    {run_long<LongShape<128, 128, 2, 2, 2>>, 128, 128, 128, 1, kAll, false, 4.18f, 0.591f, 1.22f, 0.822f},
+    {run_long<LongShape<128, 128, 2, 4, 4>>, 128, 128, 128, 1, kAll, false, 3.63f, 0.583f, 2.34f, 0.922f},
 };
 const Kernel kDirect[] = {
-    {run_tile<Shape<true, 256, 256, 2, 4, 2>>, 256, 256, 128, 1, kAll, false, 5.94f, 1.89f, 7.01f, 2.67f},
-    {run_tile<Shape<true, 128, 128, 2, 2, 2>>, 128, 128, 128, 1, kAll, false, 4.4f, 0.938f, 1.75f, 0.971f},
-    {run_tile<Shape<true, 128, 128, 2, 4, 4>>, 128, 128, 128, 1, kAll, false, 3.82f, 0.745f, 2.54f, 1.07f},
-    {run_tile<Shape<true, 128, 64, 4, 2, 3>>, 128, 64, 128, 1, kAll, true, 0.566f, 0.699f, 2.99f, 0.55f},
-    {run_tile<Shape<true, 64, 64, 2, 2, 4>>, 64, 64, 128, 1, kAll, true, 2.46f, 0.356f, 0.881f, 0.319f},
-    {run_tile<Shape<true, 32, 64, 1, 4, 4, 2>>, 32, 64, 128, 2, kAll, true, 1.13f, 0.556f, 2.18f, 0.469f},
-    {run_tile<Shape<true, 32, 32, 2, 2, 6, 2>>, 32, 32, 128, 2, kAll, true, 1.38f, 0.469f, 1.78f, 0.35f},
-    {run_thin<4>, 16, 16, 256, 4, 300, true, 2.63f, 0.778f, 0.f, 0.605f},
+    {run_tile<Shape<true, 256, 256, 2, 4, 2>>, 256, 256, 128, 1, kAll, false, 6.14f, 1.76f, 9.48f, 2.71f},
+    {run_tile<Shape<true, 128, 128, 2, 2, 2>>, 128, 128, 128, 1, kAll, false, 4.36f, 0.97f, 2.06f, 0.939f},
+    {run_tile<Shape<true, 128, 128, 2, 4, 4>>, 128, 128, 128, 1, kAll, false, 3.95f, 0.751f, 2.98f, 1.07f},
+    {run_tile<Shape<true, 128, 64, 4, 2, 3>>, 128, 64, 128, 1, kAll, true, 1.4f, 0.34f, 2.43f, 0.562f},
+    {run_tile<Shape<true, 64, 64, 2, 2, 4>>, 64, 64, 128, 1, kAll, false, 3.78f, 0.279f, 0.594f, 0.383f},
+    {run_tile<Shape<true, 32, 64, 1, 4, 4, 2>>, 32, 64, 128, 2, kAll, false, 3.58f, 0.409f, 1.22f, 0.688f},
+    {run_tile<Shape<true, 32, 32, 2, 2, 6, 2>>, 32, 32, 128, 2, kAll, true, 1.66f, 0.432f, 1.84f, 0.337f},
+    {run_thin<4>, 16, 16, 256, 4, 300, true, 2.53f, 0.801f, 0.f, 0.667f},
 };
 const Kernel kAny[] = {
-    {run_tile<Shape<false, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, kAll, true, 0.368f, 1.48f, 4.3f, 1.18f},
-    {run_tile<Shape<false, 128, 64, 4, 2, 2>>, 128, 64, 128, 1, kAll, true, 0.773f, 1.13f, 3.44f, 0.857f},
-    {run_tile<Shape<false, 64, 64, 2, 4, 2>>, 64, 64, 128, 1, kAll, true, 1.08f, 0.711f, 2.49f, 0.616f},
-    {run_tile<Shape<false, 32, 64, 1, 4, 2, 2>>, 32, 64, 128, 2, kAll, true, 1.25f, 0.913f, 2.75f, 0.778f},
-    {run_tile<Shape<false, 32, 32, 2, 2, 2, 2>>, 32, 32, 128, 2, kAll, true, 2.68f, 0.447f, 0.891f, 0.51f},
-    {run_thin<4>, 16, 16, 256, 4, 300, true, 2.29f, 1.87f, 0.f, 1.09f},
+    {run_tile<Shape<false, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, kAll, true, 0.634f, 1.42f, 4.16f, 1.21f},
+    {run_tile<Shape<false, 128, 64, 4, 2, 2>>, 128, 64, 128, 1, kAll, true, 1.36f, 1.04f, 3.07f, 0.891f},
+    {run_tile<Shape<false, 64, 64, 2, 2, 2>>, 64, 64, 128, 1, kAll, true, 3.42f, 0.578f, 1.21f, 0.525f},
+    {run_tile<Shape<false, 32, 64, 1, 4, 2, 2>>, 32, 64, 128, 2, kAll, true, 1.6f, 0.039f, 2.74f, 0.737f},
+    {run_tile<Shape<false, 32, 32, 2, 2, 2, 2>>, 32, 32, 128, 2, kAll, true, 3.05f, 0.543f, 0.804f, 0.49f},
+    {run_thin<4>, 16, 16, 256, 4, 300, true, 2.18f, 2.f, 0.f, 1.12f},
 };
 
 int run_product4(const Product4 &p, hipStream_t stream)
@@ -695,8 +696,10 @@ int run_product4(const Product4 &p, hipStream_t stream)
     float least = 0.f;
     const auto consider = [&](const Kernel &k) {
         if (rows > k.most) return;
-        const int64_t groups = parts * ((rows + k.bm - 1) / k.bm) * ((p.n + k.bn - 1) / k.bn), slabs = (p.k + k.step - 1) / k.step;
-        const float steps = (float)((slabs + k.ways - 1) / k.ways), load = k.round_up ? (float)((groups + 255) / 256) : (float)groups / 256.f;
+        // experts' rows end anywhere in a tile: half a tile more each
+        const float down = p.offsets ? parts * std::max(1.f, (float)rows / k.bm + 0.5f) : (float)((rows + k.bm - 1) / k.bm), groups = down * (float)((p.n + k.bn - 1) / k.bn);
+        const int64_t slabs = (p.k + k.step - 1) / k.step;
+        const float steps = (float)((slabs + k.ways - 1) / k.ways), load = k.round_up ? std::ceil(groups / 256.f) : groups / 256.f;
         const float us = k.launch + std::max(steps * k.chain, load * (k.tile + steps * k.rate));
         if (!best || us < least) { best = &k; least = us; }
     };

@@ -24,6 +24,16 @@ template <typename T> struct Vec {
     T v[n];
 };
 
+// Stores 16 bytes that no kernel before the end of this one reads: they leave for memory at once, where lines left in the L2s are written back at the end of the launch.
+// Every address takes them.
+__device__ __forceinline__ void store_away(void *to, const void *from)
+{
+    typedef int any __attribute__((ext_vector_type(4), aligned(1)));
+    any v;
+    __builtin_memcpy(&v, from, 16);
+    __builtin_nontemporal_store(v, static_cast<any *>(to));
+}
+
 using opevo::fail;
 
 inline bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }

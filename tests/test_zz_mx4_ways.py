@@ -16,6 +16,7 @@ from test_zz_experts_ways import _compile, _cut, _source
 def _chooser(tmp_path):
     """The kernels of the tables by numbers of their own, and the one that is chosen for a size."""
     lib = _compile(tmp_path, """
+#include <cmath>
 typedef void *hipStream_t;
 struct Product4 { const uint8_t *a, *b, *sa, *sb; long lda, ldb, ldsa, ldsb; const int *offsets; int experts; long m; int n, k; bool odd; };
 template <bool DIRECT, int BM, int BN, int WM, int WN, int STAGES, int KG = 1> struct Shape { static constexpr int id = ((DIRECT * 1000 + BM) * 1000 + BN) * 100 + STAGES * 10 + KG; };
@@ -60,10 +61,11 @@ GROUPS = [
     ([3, 0, 5, 1], 2, 520, 1280, "f32"), ([2, 1, 0, 6], 1, 77, 333, "f16"),
     ([2600, 0, 4000, 3000, 2700, 3800], 46, 21, 256, "bf16"), ([20, 0, 31, 14, 18], 2, 3271, 1024, "f32"), ([17, 20, 14, 0, 30, 20], 1, 2739, 4096, "f16"), ([65, 130, 0, 100, 60, 30], 5, 2692, 256, "f32"),
     ([134, 200, 0, 166, 160], 10, 3274, 256, "bf16"),
+    ([40, 0, 90, 62, 55, 38], 3, 2935, 1024, "bf16"), ([3000, 2000, 0, 6000], 4, 202, 256, "f16"), ([2700, 3100, 0, 5000, 2600, 2800], 6, 66, 640, "f32"),
 ]
 
 
-PLAIN = [(1361, 1531, 2048, "bf16"), (863, 1503, 4096, "f32")]
+PLAIN = [(2949, 3460, 2048, "f16"), (1361, 1531, 2048, "bf16"), (863, 1503, 4096, "f32")]
 
 
 def test_every_kernel_of_the_products_is_chosen_plain_and_by_experts(tmp_path):
