@@ -160,8 +160,8 @@ void product4_thin(Product4 p)
 
 // ------------------------------------------------------------------ tiles
 // Workgroup tile BM x BN, slabs of 128 bytes (256 values), WM x WN waves of MI x NI atoms of 16 x 16 x 128, KG groups of such waves that take every KG-th slab and add up
-// their sums in LDS at the end.  The 16-byte chunk c of a row sits at chunk position c ^ (row / 2 % 8) of its row of the slab: the 16 lanes of a turn of a fragment read then
-// fall on 16 different groups of banks.  Behind the rows of a slab stand their factors, eight bytes a row.  Rows past the end repeat the last one (their results are not stored); chunks past K are zeros.
+// their sums in LDS at the end.  The 16-byte chunk 2 g + kk of a row, which group g of lanes reads in step kk, sits at chunk position (g + 4 kk) ^ (row / 2 % 8) of its row of the slab: the lanes of
+// a turn of a fragment read then fall on different groups of banks (with (2 g + kk) ^ ... half of the LDS cycles were conflicts).  Behind the rows of a slab stand their factors, eight bytes a row.  Rows past the end repeat the last one (their results are not stored); chunks past K are zeros.
 // DIRECT: every wave issues wave-wide loads whose destination is LDS (16 bytes a lane for the codes, the chunk each lane loads chosen by the permutation, 4 for the factors); a
 // ring of STAGES slabs keeps STAGES - 1 in flight.  For operands whose pointers and row lengths are multiples of 16 (factors: of 4) and K of 32.
 // Otherwise the slabs pass through registers, from where they start on any address: two stages in LDS, the slab after them on its way.
@@ -177,6 +177,13 @@ struct Shape {
                       && BYTES <= 160 * 1024 && NW * KG <= 16 && BM + BN <= NW * 64 && STAGE % 16 == 0,
                   "");
 };
+
+// The chunk at a position of a row.
+__device__ __forceinline__ int chunk_for(int position, int row)
+{
+    const int at = position ^ (row >> 1 & 7);
+    return (at & 3) << 1 | at >> 2;
+}
 
 // lane i's 4 bytes from base + off to LDS at lds + 4 i, as load_to_lds.
 __device__ __forceinline__ void load_word_to_lds(const int8_t *base, unsigned off, unsigned lds)
@@ -207,7 +214,7 @@ void product4_tile(Product4 p)
         for (int t = 0; t < PER; ++t) {
             const bool is_a = t < LA;
             const int row = (is_a ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, limit = is_a ? rows : cols;
-            const int chunk = (lane & 7) ^ (row >> 1 & 7);
+            const int chunk = chunk_for(lane & 7, row);
             off[t] = (unsigned)(row < limit ? row : limit - 1) * (unsigned)(is_a ? p.lda : p.ldb) + chunk * 16;
         }
         const long b0 = (long)r.expert * p.n + n0;
@@ -241,7 +248,7 @@ void product4_tile(Product4 p)
             const unsigned at = ring_at + stage * S::STAGE, at_a = at + wave * LA * 1024, at_b = at + BM * BK + wave * LB * 1024;
 #pragma unroll
             for (int t = 0; t < PER; ++t) {
-                const int row = (t < LA ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, chunk = (lane & 7) ^ (row >> 1 & 7);
+                const int row = (t < LA ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, chunk = chunk_for(lane & 7, row);
                 const unsigned to = t < LA ? at_a + t * 1024 : at_b + (t - LA) * 1024;
                 if (slab * BK + chunk * 16 < p.k) load_to_lds(t < LA ? as : bs, off[t], to);
                 else *(i32x4 *)(ring + (to - ring_at) + lane * 16) = i32x4{0, 0, 0, 0};
@@ -265,7 +272,7 @@ void product4_tile(Product4 p)
             const int slab = step * S::KG + group;
 #pragma unroll
             for (int t = 0; t < PER; ++t) {
-                const int row = (t < LA ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, chunk = (lane & 7) ^ (row >> 1 & 7);
+                const int row = (t < LA ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, chunk = chunk_for(lane & 7, row);
                 hold[t] = load_codes((const uint8_t *)(t < LA ? abase : bbase) + off[t] - chunk * 16, slab * BK + chunk * 16, p.k, p.odd);
             }
             const uint8_t *of = (const uint8_t *)(mine < BM ? afact : bfact) + factors_at(mine);
@@ -315,7 +322,7 @@ void product4_tile(Product4 p)
         };
         // fragments: lane l holds row l % 16, and of the step kk the 32 values from 64 * (l / 16) + 32 kk on; both steps' factors in a word
         const int sw = lane >> 1 & 7, fr = lane & 15, g = lane >> 4;
-        auto chunk_at = [&](int stage, int kk) { return ring + stage * S::STAGE + ((g * 2 + kk ^ sw) << 4); };
+        auto chunk_at = [&](int stage, int kk) { return ring + stage * S::STAGE + ((g + 4 * kk ^ sw) << 4); };
         auto read_factor = [&](int stage, int row) { return (int)*(const uint16_t *)(ring + stage * S::STAGE + S::CODES + (row + fr) * 8 + g * 2); };
         // prologue: slabs 0 .. STAGES - 1 under way, slab 0 landed, its first fragments read
         if (!S::DIRECT) {
@@ -503,7 +510,7 @@ void product4_long(Product4 p)
             const int row = (is_a ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8;
             off[t] = (unsigned)min(row, (is_a ? rows : cols) - 1) * (unsigned)(is_a ? p.lda : p.ldb);
             asm("" : "+v"(off[t]));         // product and sum in one instruction would take, and keep, two registers
-            off[t] += ((lane & 7) ^ (row >> 1 & 7)) * 16;
+            off[t] += chunk_for(lane & 7, row) * 16;
         }
         int half[S::FPER], first[S::FPER];
 #pragma unroll
@@ -536,8 +543,8 @@ void product4_long(Product4 p)
         unsigned at_a[2], at_b[2], at_fa = sets_at + (wm * MI * 16 + fr) * 16 + g * 2, at_fb = sets_at + (BM + wn * NI * 16 + fr) * 16 + g * 2;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
-            at_a[kk] = ring_at + (wm * MI * 16 + fr) * BK + ((g * 2 + kk ^ sw) << 4);
-            at_b[kk] = ring_at + (BM + wn * NI * 16 + fr) * BK + ((g * 2 + kk ^ sw) << 4);
+            at_a[kk] = ring_at + (wm * MI * 16 + fr) * BK + ((g + 4 * kk ^ sw) << 4);
+            at_b[kk] = ring_at + (BM + wn * NI * 16 + fr) * BK + ((g + 4 * kk ^ sw) << 4);
         }
         i32x4 af[R], bf[2][NI];
         int fa[MI], fb[2][NI];
