@@ -112,7 +112,7 @@ void product4_thin(Product4 p)
         i32x4 v[2][4], w[2][4], fv[2], fw[2];
         auto load = [&](i32x4 (&to)[2][4], i32x4 (&f)[2], int step) {
             const int k0 = step * 256 + g * 16;
-            if (step * 256 + 256 <= p.k && !p.odd) {
+            if (step * 256 + 256 <= (p.odd ? p.k - 1 : p.k)) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     __builtin_memcpy(&f[i], by[i] + step * 16, 16);
@@ -120,13 +120,17 @@ void product4_thin(Product4 p)
                     for (int u = 0; u < 4; ++u) __builtin_memcpy(&to[i][u], row[i] + k0 + u * 64, 16);
                 }
             } else {
+                auto end = [&](auto is_long) __attribute__((always_inline)) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                    for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        f[i][u] = load_factors(by[i], step * 16 + u * 4, p.blocks);
-                        to[i][u] = load_codes(row[i], k0 + u * 64, p.k, p.odd);
-                    }
+                        for (int u = 0; u < 4; ++u) {
+                            f[i][u] = load_factors<decltype(is_long)::value>(by[i], step * 16 + u * 4, p.blocks);
+                            to[i][u] = load_codes<decltype(is_long)::value>(row[i], k0 + u * 64, p.k, p.odd);
+                        }
+                };
+                if (p.blocks >= 4) end(std::true_type());
+                else end(std::false_type());
             }
         };
         auto multiply = [&](const i32x4 (&of)[2][4], const i32x4 (&f)[2]) {
@@ -254,9 +258,11 @@ void product4_tile(Product4 p)
                 else *(i32x4 *)(ring + (to - ring_at) + lane * 16) = i32x4{0, 0, 0, 0};
             }
 #pragma unroll
-            for (int t = 0; t < S::FPER; ++t)
-                *(int *)(ring + stage * S::STAGE + S::CODES + fpiece[t] * 256 + lane * 4) =
-                    load_factors((const uint8_t *)(fpiece[t] < BM / 32 ? afact : bfact) + (foff[t] - (lane & 1) * 4), slab * 8 + (lane & 1) * 4, p.blocks);
+            for (int t = 0; t < S::FPER; ++t) {
+                const uint8_t *of = (const uint8_t *)(fpiece[t] < BM / 32 ? afact : bfact) + (foff[t] - (lane & 1) * 4);
+                const int b = slab * 8 + (lane & 1) * 4;
+                *(int *)(ring + stage * S::STAGE + S::CODES + fpiece[t] * 256 + lane * 4) = p.blocks >= 4 ? load_factors<true>(of, b, p.blocks) : load_factors<false>(of, b, p.blocks);
+            }
         };
         // The same by way of registers: fetch starts the loads, put stores what they brought.  A thread takes the factors of one row.
         i32x4 hold[PER];
@@ -268,16 +274,21 @@ void product4_tile(Product4 p)
             for (int t = 0; t < PER; ++t) __builtin_memcpy(&hold[t], (t < LA ? abase : bbase) + (long)slab * BK + off[t], 16);
             __builtin_memcpy(fhold, (mine < BM ? afact : bfact) + factors_at(mine) + (long)slab * 8, 8);
         };
-        auto fetch_ragged = [&](int step) {
+        auto fetch_end = [&](auto is_long, int step) __attribute__((always_inline)) {
+            constexpr bool LONG = decltype(is_long)::value;
             const int slab = step * S::KG + group;
 #pragma unroll
             for (int t = 0; t < PER; ++t) {
                 const int row = (t < LA ? wave * LA + t : wave * LB + t - LA) * 8 + lane / 8, chunk = chunk_for(lane & 7, row);
-                hold[t] = load_codes((const uint8_t *)(t < LA ? abase : bbase) + off[t] - chunk * 16, slab * BK + chunk * 16, p.k, p.odd);
+                hold[t] = load_codes<LONG>((const uint8_t *)(t < LA ? abase : bbase) + off[t] - chunk * 16, slab * BK + chunk * 16, p.k, p.odd);
             }
             const uint8_t *of = (const uint8_t *)(mine < BM ? afact : bfact) + factors_at(mine);
-            fhold[0] = load_factors(of, slab * 8, p.blocks);
-            fhold[1] = load_factors(of, slab * 8 + 4, p.blocks);
+            fhold[0] = load_factors<LONG>(of, slab * 8, p.blocks);
+            fhold[1] = load_factors<LONG>(of, slab * 8 + 4, p.blocks);
+        };
+        auto fetch_ragged = [&](int step) __attribute__((always_inline)) {
+            if (p.blocks >= 4) fetch_end(std::true_type(), step);
+            else fetch_end(std::false_type(), step);
         };
         auto put = [&](int stage) {
 #pragma unroll
@@ -656,7 +667,7 @@ int run_thin(const Product4 &p, hipStream_t stream)
 // A kernel and what it takes, in us: launch + max(steps * chain, load * (tile + steps * rate)), where steps is how many slabs (thin: steps of 256 bytes) a wave
 // goes through and load the workgroups for each of the 256 compute units, rounded up where that foretold the times better.  The first term is a workgroup's chain of latencies,
 // the second what a compute unit gets through.  The constants were fitted to the times of every kernel at 750 random sizes of 1 - 8192 rows, 64 - 8192 columns and K of 64 - 8192 (a third
-// each of K in multiples of 1024, of 32, and any), those near the best one's counting most; the kernel chosen by them took 2.3, 2.8 and 1.8 % more than the best of all
+// each of K in multiples of 1024, of 32, and any), those near the best one's counting most; the kernel chosen by them took 2.3, 2.8 and 1.7 % more than the best of all
 // in the geometric mean, at most 1.9 times as much.  By experts they are used with the tiles that an even deal of the rows would make.
 struct Kernel {
     int (*run)(const Product4 &, hipStream_t);
@@ -684,7 +695,7 @@ const Kernel kDirect[] = {
 const Kernel kAny[] = {
     {run_tile<Shape<false, 128, 128, 2, 4, 2>>, 128, 128, 128, 1, kAll, true, 0.634f, 1.42f, 4.16f, 1.21f},
     {run_tile<Shape<false, 128, 64, 4, 2, 2>>, 128, 64, 128, 1, kAll, true, 1.36f, 1.04f, 3.07f, 0.891f},
-    {run_tile<Shape<false, 64, 64, 2, 2, 2>>, 64, 64, 128, 1, kAll, true, 3.42f, 0.578f, 1.21f, 0.525f},
+    {run_tile<Shape<false, 64, 64, 2, 4, 2>>, 64, 64, 128, 1, kAll, false, 4.05f, 0.479f, 1.28f, 0.846f},
     {run_tile<Shape<false, 32, 64, 1, 4, 2, 2>>, 32, 64, 128, 2, kAll, true, 1.6f, 0.039f, 2.74f, 0.737f},
     {run_tile<Shape<false, 32, 32, 2, 2, 2, 2>>, 32, 32, 128, 2, kAll, true, 3.05f, 0.543f, 0.804f, 0.49f},
     {run_thin<4>, 16, 16, 256, 4, 300, true, 2.18f, 2.f, 0.f, 1.12f},

@@ -23,16 +23,33 @@ __device__ __forceinline__ i32x4 without_half_byte(i32x4 v, int k, int end, bool
             if (last >> 2 == i) v[i] &= ~(0xf0 << 8 * (last & 3));
     return v;
 }
-// 16 bytes of a row from byte k on, zeros past its end (and in the half byte past an odd K).
-__device__ __forceinline__ i32x4 load_codes(const uint8_t *row, int k, int end, bool odd) { return without_half_byte(load_chunk((const int8_t *)row, k, end), k, end, odd); }
-// Four factors of a row from block b on, zeros past its end: with codes of zero any factor but NaN gives zero.
-__device__ __forceinline__ int load_factors(const uint8_t *row, int b, int blocks)
+// 16 bytes of a row from byte k on, a multiple of 16, zeros past its end (and in the half byte past an odd K).  LONG: of a row of 16 bytes or more, without a branch, so that the latencies of
+// several overlap: the piece that the row ends in comes as its last 16 bytes, shifted.
+template <bool LONG> __device__ __forceinline__ i32x4 load_codes(const uint8_t *row, int k, int end, bool odd)
 {
-    int v = 0;
+    if (!LONG) return without_half_byte(load_chunk((const int8_t *)row, k, end), k, end, odd);
+    i32x4 v, w;
+    __builtin_memcpy(&v, row + min(k, end - 16), 16);
+    const int by = (16 - end % 16) % 16;                    // alike for all lanes
+    w = by & 8 ? i32x4{v[2], v[3], 0, 0} : v;
+    w = by & 4 ? i32x4{w[1], w[2], w[3], 0} : w;
+    w = i32x4{(int)__builtin_amdgcn_alignbyte(w[1], w[0], by), (int)__builtin_amdgcn_alignbyte(w[2], w[1], by), (int)__builtin_amdgcn_alignbyte(w[3], w[2], by), (int)__builtin_amdgcn_alignbyte(0, w[3], by)};
+    w = k < end ? w : i32x4{0, 0, 0, 0};
+    return without_half_byte(k + 16 <= end ? v : w, k, end, odd);
+}
+// Four factors of a row from block b on, zeros past its end: with codes of zero any factor but NaN gives zero.  LONG: of a row of four or more, without a branch.
+template <bool LONG> __device__ __forceinline__ int load_factors(const uint8_t *row, int b, int blocks)
+{
+    unsigned v = 0;
+    if (LONG) {
+        const int at = min(b, blocks - 4);
+        __builtin_memcpy(&v, row + at, 4);
+        return b - at >= 4 ? 0 : (int)(v >> 8 * (b - at));
+    }
     if (b + 4 <= blocks) __builtin_memcpy(&v, row + b, 4);
     else
-        for (int i = 0; b + i < blocks; ++i) v |= (int)row[b + i] << 8 * i;
-    return v;
+        for (int i = 0; b + i < blocks; ++i) v |= (unsigned)row[b + i] << 8 * i;
+    return (int)v;
 }
 
 }  // namespace
