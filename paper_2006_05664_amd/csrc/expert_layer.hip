@@ -181,8 +181,8 @@ template <typename T> __device__ __forceinline__ bf16x8 operand(const T (&v)[8],
 
 // A lane's row of activations.  A lane without one (`on` is false) loads nothing and multiplies what its registers hold: a column of the product is its row's alone.  (Loading some row instead
 // costs as much as a row of its own: 32 tokens x 4 of 4096 x 1024, second launch, 49 us instead of 42.)
-// ORDERED: values as place_in_h puts them, rows of whole iterations.  Else `last` is a copy of an iteration that the row ends in, filled up with zeros, in the LDS.
-template <typename T, int SUB, bool ORDERED> struct Activations {
+// `last` is a copy of an iteration that the row ends in, filled up with zeros, in the LDS.
+template <typename T, int SUB> struct Activations {
     struct Raw { T v[SUB][4][8]; };
     const T *row, *last;
     int part, k;
@@ -193,12 +193,11 @@ template <typename T, int SUB, bool ORDERED> struct Activations {
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) __builtin_memcpy(r.v[u][j], row + k0 + u * kStep + (ORDERED ? j * 32 + g * 8 : g * 32 + j * 8), sizeof r.v[u][j]);
+            for (int j = 0; j < 4; ++j) __builtin_memcpy(r.v[u][j], row + k0 + u * kStep + g * 32 + j * 8, sizeof r.v[u][j]);
     }
     // the last iteration of a row that ends inside it, from the copy of it
-    __device__ __forceinline__ void load_last(Raw &r, int k0, int g) const
+    __device__ __forceinline__ void load_last(Raw &r, int g) const
     {
-        if (ORDERED) return load(r, k0, g);
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -208,12 +207,12 @@ template <typename T, int SUB, bool ORDERED> struct Activations {
 
 // The iterations first, first + stride, ... along K, the last one of which may be ragged; the wave whose turn it is takes that one.  The weights of the next iteration come from memory meanwhile; the
 // activations, of the same one, from the caches: they are asked for first, because loads are waited for in their order.
-template <Ending ENDING, bool ORDERED, typename Q, typename T, int NI>
-__device__ __forceinline__ void multiply(const Q (&w)[NI], const Activations<T, Q::SUB, ORDERED> &x, int first, int stride, int g, f32x4 (&acc)[NI])
+template <Ending ENDING, typename Q, typename T, int NI>
+__device__ __forceinline__ void multiply(const Q (&w)[NI], const Activations<T, Q::SUB> &x, int first, int stride, int g, f32x4 (&acc)[NI])
 {
     constexpr int LONG = Q::SUB * kStep;
     typedef typename Q::Raw W;
-    typedef typename Activations<T, Q::SUB, ORDERED>::Raw X;
+    typedef typename Activations<T, Q::SUB>::Raw X;
     const int whole = x.k / LONG;
     auto load = [&](W (&wr)[NI], int it) {
 #pragma unroll
@@ -236,19 +235,45 @@ __device__ __forceinline__ void multiply(const Q (&w)[NI], const Activations<T, 
     auto step = [&](const W (&wr)[NI], W (&next)[NI], int it) {
         X xr;
         x.load(xr, it * LONG, g);
-        if (it + stride < whole) load(next, it + stride);
+        load(next, it + stride);
         use(wr, xr);
     };
     W wa[NI], wb[NI];
-    int it = first;
-    if (it < whole) load(wa, it);
-    for (; it < whole; it += 2 * stride) {
-        step(wa, wb, it);
-        if (it + stride < whole) step(wb, wa, it + stride);
+    // no load of weights in the loop stands behind a branch: a wait would be for those behind it too
+    int it = first, left = first < whole ? (whole - first + stride - 1) / stride : 0;
+    if constexpr (Parts<T>::n > 1 && Q::SUB == 2) {
+        // one body where it is long, as its instructions have to come from memory too (4-bit weights, 1 token of 1967 x 768
+        // in fp32 18 us, with three bodies 20; 102 x 2 of 8 experts, 246 x 2879 in fp16 53 and 61); past the last weights those again
+        if (left > 0) load(wa, it);
+        for (; left > 0; --left) {
+            const int next = left > 1 ? it + stride : it;
+            X xr;
+            x.load(xr, it * LONG, g);
+            load(wb, next);
+            use(wa, xr);
+#pragma unroll
+            for (int n = 0; n < NI; ++n) wa[n] = wb[n];
+            it = next;
+        }
+    } else if (left > 0) {
+        load(wa, it);
+        for (; left >= 3; left -= 2, it += 2 * stride) {
+            step(wa, wb, it);
+            step(wb, wa, it + stride);
+        }
+        if (left == 2) {
+            step(wa, wb, it);
+            it += stride;
+#pragma unroll
+            for (int n = 0; n < NI; ++n) wa[n] = wb[n];
+        }
+        X xr;
+        x.load(xr, it * LONG, g);
+        use(wa, xr);
     }
     if (ENDING != kEven && whole % stride == first) {
         X xr;
-        x.load_last(xr, whole * LONG, g);
+        x.load_last(xr, g);
 #pragma unroll
         for (int n = 0; n < NI; ++n) w[n].template load_last<ENDING>(wa[n], whole * LONG, g);
         use(wa, xr);
@@ -385,7 +410,7 @@ void layer_in(Layer p)
     Q w[NI];
 #pragma unroll
     for (int n = 0; n < NI; ++n) w[n].at(p.win, p.ld_in, p.sin, p.ld_sin, first + (n < NP ? 0 : p.inner) + min(c0 + n % NP * 16 + r, p.inner - 1), p.width);
-    Activations<T, Q::SUB, false> x;
+    Activations<T, Q::SUB> x;
     x.on = r < unit.rows * PX;
     x.row = (const T *)p.x + token[min(r / PX, unit.rows - 1)] * p.ld_x;
     x.part = r % PX;
@@ -400,7 +425,7 @@ void layer_in(Layer p)
         x.last = last[min(r / PX, unit.rows - 1)];
     }
     f32x4 acc[NI] = {};
-    multiply<ENDING, false, Q, T, NI>(w, x, wave, W, g, acc);
+    multiply<ENDING, Q, T, NI>(w, x, wave, W, g, acc);
 #pragma unroll
     for (int n = 0; n < NI; ++n) sums[wave][n][lane] = acc[n];
     __syncthreads();
@@ -432,28 +457,31 @@ void layer_in(Layer p)
 }
 
 // ------------------------------------------------------------------ the second launch
-// y of COLS = 16 / S columns for a group of tokens: a task is a unit of rows of an expert and a share of K, the W waves deal the tasks among themselves, what they find for each row
+// y of NC tiles of COLS = 16 / S columns for a group of tokens: a task is a unit of rows of an expert and a share of K, the W waves deal the tasks among themselves, what they find for each row
 // meets in LDS, and the rows of a token are added up there in the order of its slots.  A wave goes through its tasks' iterations as one sequence, the next two on their way from memory whichever task
 // they belong to: an iteration is a few microseconds' worth of latency and a fraction of one of work.
 // S > 1, for few columns: K falls into S parts, and the 16 rows of weights of a product are COLS columns in each of the parts, the 16 rows of h COLS rows in each of
 // them.  Of the product the S blocks of a part with itself are used; a wave reads as much as ever, and there are S times as many workgroups.
-// Of the same layers: 73 MB in 30 - 32 us, 8.8 MB in 6.7.
+// Of the same layers: 73 MB in 27 - 28 us, 8.8 MB in 6.7 - 7.5.
 constexpr int kShares = 1024;           // rows of 16 sums in the LDS
+constexpr unsigned kNowhere = 0xf0000000u;      // behind the end of h, which has 3 * 2^30 bytes at most, with whatever is added to it
 
-template <typename T, typename Q, int W, int S, Ending ENDING>
+template <typename T, typename Q, int W, int S, int NC, Ending ENDING>
 __global__ __launch_bounds__(W * 64)
 void layer_out(Layer p)
 {
-    constexpr int NT = W * 64, COLS = 16 / S, PH = Parts<T>::h, PER = COLS / PH, LONG = Q::SUB * kStep;
-    static_assert(PER >= 1 && (S == 1 || ENDING == kEven), "");
+    constexpr int NT = W * 64, COLS = 16 / S, WIDE = NC * COLS, PH = Parts<T>::h, PER = COLS / PH, LONG = Q::SUB * kStep;
+    static_assert(PER >= 1 && (S == 1 || (ENDING == kEven && NC == 1)), "");
     __shared__ int place[kMaxSlots];
+    __shared__ float by[kMaxSlots];
     __shared__ Unit units[kMaxSlots];
-    __shared__ __attribute__((aligned(16))) float z[kShares * S][COLS];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15, part = r / COLS, c = r % COLS, n0 = blockIdx.x * COLS;
+    __shared__ __attribute__((aligned(16))) float z[kShares * S][WIDE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15, part = r / COLS, c = r % COLS, n0 = blockIdx.x * WIDE;
     const int t0 = blockIdx.y * p.group_tokens, tokens = min(p.group_tokens, p.tokens - t0), first = t0 * p.k;
     const int all = __builtin_amdgcn_readfirstlane(p.plan->units_of[blockIdx.y]), here = __builtin_amdgcn_readfirstlane(p.plan->rows_of[blockIdx.y]);
     for (int s = threadIdx.x; s < tokens * p.k; s += NT) {
         place[s] = p.plan->place[first + s];
+        by[s] = p.weight ? p.weight[first + s] : 1.f;
         units[s] = p.plan->units[first + s];
     }
     __syncthreads();
@@ -466,83 +494,116 @@ void layer_out(Layer p)
     }
     const int shift = __builtin_ctz(shares), tasks = all * shares;
 
-    // The sequence of this wave's iterations, as it is loaded and as it is used.
-    struct Place { int task, it; };
-    auto begin = [&](int task) { return Place{task, task & (shares - 1)}; };
-    Place load_at = begin(wave), use_at = load_at;
-    Q w;
-    Activations<__bf16, Q::SUB, true> x;
-    x.part = 0;
-    x.k = length;
-    x.last = nullptr;
+    // The wave's tasks, every W-th, all of the same share of K, and their iterations: as they are loaded and as they are used.
+    const int share = wave & (shares - 1), own = (tasks - wave + W - 1) / W;
+    int load_task = wave, load_it = share, use_task = wave, use_it = share;
+    Q w[NC];
+    // rows of h as a buffer, whose bounds answer for lanes without a row: zeros, and no access
+    const __amdgpu_buffer_rsrc_t h = __builtin_amdgcn_make_buffer_rsrc(p.h, 0, (int)(unsigned)((long)p.slots * PH * p.ld_h * 2), 0x00027000);
+    unsigned row_at = 0;
     auto aim = [&](int task) {
         const Unit unit = units[task >> shift];
         const int e = __builtin_amdgcn_readfirstlane(unit.expert), base = __builtin_amdgcn_readfirstlane(unit.base), rows = __builtin_amdgcn_readfirstlane(unit.rows);
-        w.at(p.wout, p.ld_out, p.sout, p.ld_sout, (long)e * p.width + min(n0 + c, p.width - 1), p.inner);
-        if (S > 1) w.skip(part * length);
-        x.on = c < rows * PH;
-        x.row = p.h + ((long)(base + min(c / PH, rows - 1)) * PH + c % PH) * p.ld_h + part * length;
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            w[n].at(p.wout, p.ld_out, p.sout, p.ld_sout, (long)e * p.width + min(n0 + n * COLS + c, p.width - 1), p.inner);
+            if (S > 1) w[n].skip(part * length);
+        }
+        row_at = c < rows * PH ? (((base + c / PH) * PH + c % PH) * (unsigned)p.ld_h + part * length + g * 8) * 2 : kNowhere;
     };
-    struct Buffer { typename Q::Raw w; typename Activations<__bf16, Q::SUB, true>::Raw x; } b0, b1, b2;
+    struct Buffer { typename Q::Raw w[NC]; i32x4 x[Q::SUB][4]; } b0, b1, b2;
     auto load = [&](Buffer &b) {
-        if (load_at.task >= tasks) return;
-        x.load(b.x, load_at.it * LONG, g);
-        if (ENDING == kEven || load_at.it < whole) w.load(b.w, load_at.it * LONG, g);
-        else w.template load_last<ENDING>(b.w, load_at.it * LONG, g);
-        load_at.it += shares;
-        if (load_at.it >= count) {
-            load_at = begin(load_at.task + W);
-            if (load_at.task < tasks) aim(load_at.task);
+#pragma unroll
+        for (int u = 0; u < Q::SUB; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b.x[u][j] = __builtin_amdgcn_raw_buffer_load_b128(h, row_at + (load_it * LONG + u * kStep + j * 32) * 2, 0, 0);
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            if (ENDING == kEven || load_it < whole) w[n].load(b.w[n], load_it * LONG, g);
+            else w[n].template load_last<ENDING>(b.w[n], load_it * LONG, g);
+        }
+        load_it += shares;
+        if (load_it >= count && load_task + W < tasks) {
+            load_it = share;
+            load_task += W;
+            aim(load_task);
         }
     };
-    f32x4 acc = {};
+    f32x4 acc[NC] = {};
     auto use = [&](const Buffer &b) {
 #pragma unroll
         for (int u = 0; u < Q::SUB; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Q::operand(b.w, u, j, g), operand(b.x.v[u][j], 0), acc, 0, 0, 0);
-        asm volatile("" : "+v"(acc));           // due here, not behind the next branch
-        use_at.it += shares;
-        if (use_at.it < count) return;
-        const Unit unit = units[use_at.task >> shift];
-        f32x4 v;
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float sum = acc[i];
+                for (int n = 0; n < NC; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Q::operand(b.w[n], u, j, g), __builtin_bit_cast(bf16x8, b.x[u][j]), acc[n], 0, 0, 0);
 #pragma unroll
-            for (int o = 1; o < PH; ++o) sum += __shfl_down(acc[i], o);
-            v[i] = sum;
+        for (int n = 0; n < NC; ++n) asm volatile("" : "+v"(acc[n]));           // due here, not behind the next branch
+        use_it += shares;
+        if (use_it < count) return;
+        const Unit unit = units[use_task >> shift];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            f32x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float sum = acc[n][i];
+#pragma unroll
+                for (int o = 1; o < PH; ++o) sum += __shfl_down(acc[n][i], o);
+                v[i] = sum;
+            }
+            // lane (r, g) has the sums of rows 4 g .. 4 g + 3 of the weights with row r of h
+            if (g * 4 / COLS == part && c < unit.rows * PH && c % PH == 0)
+                *(f32x4 *)&z[(share * S + part) * here + unit.first + c / PH][n * COLS + g * 4 % COLS] = v;
+            acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        // lane (r, g) has the sums of rows 4 g .. 4 g + 3 of the weights with row r of h
-        if (g * 4 / COLS == part && c < unit.rows * PH && c % PH == 0) *(f32x4 *)&z[((use_at.task & (shares - 1)) * S + part) * here + unit.first + c / PH][g * 4 % COLS] = v;
-        acc = f32x4{0.f, 0.f, 0.f, 0.f};
-        use_at = begin(use_at.task + W);
+        use_it = share;
+        use_task += W;
     };
-    if (load_at.task < tasks) aim(load_at.task);
-    load(b0);
-    load(b1);
-    while (use_at.task < tasks) {
-        load(b2);
-        use(b0);
-        if (use_at.task >= tasks) break;
+    // Two iterations are on their way while one is used.  In the loop no load stands behind a branch: waits there would be for all loads, as if those behind it had not been.
+    int left = own > 0 ? own * ((count - share + shares - 1) / shares) : 0;
+    if (left > 0) aim(wave);
+    if (left >= 2) {
         load(b0);
-        use(b1);
-        if (use_at.task >= tasks) break;
         load(b1);
-        use(b2);
+        for (; left >= 5; left -= 3) {
+            load(b2);
+            use(b0);
+            load(b0);
+            use(b1);
+            load(b1);
+            use(b2);
+        }
+        if (left >= 3) load(b2);
+        use(b0);
+        if (left >= 4) load(b0);
+        use(b1);
+        if (left >= 3) use(b2);
+        if (left >= 4) use(b0);
+    } else if (left == 1) {
+        load(b0);
+        use(b0);
     }
     __syncthreads();
-    for (int o = threadIdx.x; o < tokens * COLS; o += NT) {
-        const int t = o / COLS, col = o % COLS;
+    for (int o = threadIdx.x; o < tokens * WIDE; o += NT) {
+        const int t = o / WIDE, col = o % WIDE;
         if (n0 + col >= p.width) continue;
         float y = 0.f;
-        for (int j = 0; j < p.k; ++j) {
-            const int row = place[t * p.k + j], s = first + t * p.k + j;
-            if (row < 0) continue;
-            float sum = 0.f;
-            for (int u = 0; u < shares * S; ++u) sum += z[u * here + row][col];
-            sum *= Q::scale(p.sout, (long)p.expert[s] * p.width + n0 + col);
-            y = fmaf(p.weight ? p.weight[s] : 1.f, sum, y);
+        for (int j0 = 0; j0 < p.k; j0 += 4) {           // four scales on their way
+            float scale[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int s = t * p.k + min(j0 + j, p.k - 1);
+                scale[j] = place[s] < 0 ? 0.f : Q::scale(p.sout, (long)p.expert[first + s] * p.width + n0 + col);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int s = t * p.k + j0 + j, row = j0 + j < p.k ? place[s] : -1;
+                if (row < 0) continue;
+                float sum = 0.f;
+                for (int u = 0; u < shares * S; ++u) sum += z[u * here + row][col];
+                y = fmaf(by[s], sum * scale[j], y);
+            }
         }
         ((T *)p.y)[(t0 + t) * p.ld_y + n0 + col] = narrow<T>(y);
     }
@@ -577,15 +638,19 @@ int run_layer(Layer p, hipStream_t stream)
     const int tiles = (p.width + 15) / 16;
     int parts = tiles <= 80 ? 4 : tiles <= 160 ? 2 : 1;
     while (parts > 1 && (p.inner % (parts * LONG) != 0 || 16 / parts < Parts<T>::h)) parts /= 2;
-    auto *out = of == kTiny ? layer_out<T, Q, 8, 1, kTiny> : of == kRagged ? layer_out<T, Q, 8, 1, kRagged>
-                : parts == 4 ? layer_out<T, Q, 8, 4, kEven> : parts == 2 ? layer_out<T, Q, 8, 2, kEven> : layer_out<T, Q, 8, 1, kEven>;
+    // for many slots 32 columns a workgroup, which halve what it reads of h for its weights (4 bits, 32 tokens x 4 of 64 experts, 4096 x 1024, second launch, 28 us instead of 32; 63 x 5 of 72,
+    // 2983 x 640 in fp16 101 in all instead of 122; 5 x 6 of 9, 2048 x 1868 45 instead of 36)
+    const bool wide = parts == 1 && p.slots >= 80 && p.width >= 1024;
+    auto *out = wide ? (of == kTiny ? layer_out<T, Q, 8, 1, 2, kTiny> : of == kRagged ? layer_out<T, Q, 8, 1, 2, kRagged> : layer_out<T, Q, 8, 1, 2, kEven>)
+                : of == kTiny ? layer_out<T, Q, 8, 1, 1, kTiny> : of == kRagged ? layer_out<T, Q, 8, 1, 1, kRagged>
+                : parts == 4 ? layer_out<T, Q, 8, 4, 1, kEven> : parts == 2 ? layer_out<T, Q, 8, 2, 1, kEven> : layer_out<T, Q, 8, 1, 1, kEven>;
     // ... and where that is not enough the tokens in groups, each of which reads its experts' weights again, mostly from the caches (us, one sequence of iterations and groups against neither: 4-bit
     // weights, 102 tokens x 2 of 8 experts, 246 columns of 2879 inner ones, fp16 61 / 132; 126 x 1 of 15, 469 of 1280, fp32 47 / 81; 8 bits, 32 x 1 of 62, 64 of 525 10 / 19)
-    const int cols = 16 / parts, across = (p.width + cols - 1) / cols;
+    const int cols = wide ? 32 : 16 / parts, across = (p.width + cols - 1) / cols;
     p.groups = std::min(p.tokens, std::max(1, 256 / across));
     p.group_tokens = (p.tokens + p.groups - 1) / p.groups;
     p.groups = (p.tokens + p.group_tokens - 1) / p.group_tokens;
-    p.group_unit = cols / Parts<T>::h;
+    p.group_unit = 16 / parts / Parts<T>::h;
 
     const int units = std::min(p.slots, std::min(p.slots, p.experts) + p.slots / PER);      // of the first launch; there can be no more
     const int channels = 16 * (in == kEven ? kPairs<T, Q, kEven> : kPairs<T, Q, kRagged>);

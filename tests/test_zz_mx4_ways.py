@@ -115,7 +115,7 @@ struct Weights4 { static constexpr int SUB = 2; };
 template <typename T, typename Q, Ending E> constexpr int kPairs = 2;
 static int asked[8];
 template <typename T, typename Q, int W, Ending E> void layer_in(Layer) { asked[0] = E; }
-template <typename T, typename Q, int W, int S, Ending E> void layer_out(Layer p) { asked[1] = E; asked[2] = S; asked[3] = p.groups; asked[4] = p.group_tokens; asked[5] = p.group_unit; }
+template <typename T, typename Q, int W, int S, int NC, Ending E> void layer_out(Layer p) { asked[1] = E; asked[2] = S * 10 + NC; asked[3] = p.groups; asked[4] = p.group_tokens; asked[5] = p.group_unit; }
 static int launch(const char *, void (*k)(Layer), dim3 grid, dim3, hipStream_t, Layer p) { k(p); asked[6] = asked[7]; asked[7] = grid.y; return 0; }
 """ + _cut(_source("expert_layer.hip"), "template <typename T, typename Q>\nint run_layer(") + """
 extern "C" void ask(int f32, int i8, int tokens, int k, int experts, int width, int inner, int *to)
@@ -131,7 +131,7 @@ extern "C" void ask(int f32, int i8, int tokens, int k, int experts, int width, 
         to = (ctypes.c_int * 8)()
         self.lib.ask(int(dtype == "f32"), int(kind == "i8"), tokens, k, experts, width, inner, to)
         first, second, parts, groups, each, unit, units, grid = to
-        assert grid == groups and (groups - 1) * each < tokens <= groups * each and 1 <= unit * (3 if dtype == "f32" else 2) <= 16 // parts
+        assert grid == groups and (groups - 1) * each < tokens <= groups * each and 1 <= unit * (3 if dtype == "f32" else 2) <= 16 // (parts // 10)
         return {("first", first), ("second", second, parts, "one group" if groups == 1 else "a token each" if each == 1 else "groups")}
 
 
@@ -140,6 +140,7 @@ LAYERS = [
     (3, 2, 4, 2064, 300, 1.0, 0, 0), (100, 2, 6, 2064, 1001, 0.9, 0, 0), (60, 3, 7, 4112, 512, 1.0, 0, 0), (200, 2, 5, 3000, 270, 0.9, 0, 0), (200, 1, 3, 4112, 12, 1.0, 0, 0), (9, 2, 3, 4112, 20, 1.0, 0, 0),
     (120, 4, 9, 640, 1024, 0.9, 0, 0), (300, 1, 9, 1500, 512, 0.9, 0, 0), (2, 2, 3, 2560, 1024, 1.0, 0, 0), (90, 1, 2, 200, 10, 1.0, 0, 0), (1, 3, 3, 4200, 9, 1.0, 0, 0), (5, 1, 2, 40, 14, 1.0, 0, 0),
     (1, 2, 3, 4112, 512, 1.0, 0, 0), (1, 2, 3, 4112, 270, 1.0, 0, 0), (30, 2, 3, 270, 12, 1.0, 0, 0), (70, 2, 3, 2560, 2048, 1.0, 0, 0), (1, 2, 3, 2560, 2048, 1.0, 0, 0), (20, 3, 4, 128, 512, 0.9, 0, 0),
+    (50, 2, 4, 1100, 128, 0.9, 0, 0), (50, 2, 4, 1100, 256, 1.0, 5, 1), (40, 2, 4, 4112, 100, 0.9, 0, 0), (60, 2, 3, 1030, 9, 1.0, 1, 3),
     (20, 2, 4, 130, 1024, 1.0, 0, 0), (17, 2, 4, 72, 512, 0.9, 0, 0), (5, 2, 4, 130, 1024, 1.0, 0, 0), (5, 2, 4, 130, 512, 1.0, 3, 1),
 ]
 
