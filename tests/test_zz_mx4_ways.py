@@ -275,3 +275,24 @@ def test_an_error_of_another_call_is_not_this_one_s():
     assert hip.hipGetLastError() == 0
     torch.cuda.synchronize()
     assert failed == []
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["i8", "mx4"])
+def test_the_longest_inner_rows_of_the_most_slots(kind):
+    """Rows of the layer's workspace beyond 2^31 bytes: 512 slots of 2^20 inner channels in three parts are 3 * 2^30."""
+    torch, _ = _torch()
+    tokens, width, inner, g = 512, 2, 1 << 20, torch.Generator(device="cuda").manual_seed(3)
+    win, wout = L.Weights(g, 2 * inner, width, kind), L.Weights(g, width, inner, kind)
+    xv = torch.randn(tokens, width, generator=g, device="cuda").cpu().numpy()
+    x, y = Matrix(tokens, width, "f32", values=xv), Matrix(tokens, width, "f32")
+    ids = np.zeros((tokens, 1), dtype=np.int32)
+    d_ids = torch.zeros(tokens, dtype=torch.int32, device="cuda")
+    size = P.opevo_expert_layer_workspace(tokens, 1, P.OPEVO_F32, inner)
+    assert size > 3 << 30
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    L._call(kind, x, "f32", d_ids, None, tokens, 1, 1, width, inner, win, wout, y, ws, size)
+    got, some = y.host(), np.array([0, 1, 200, 341, 342, 510, 511])
+    L._layer.dtype = "f32"
+    want, err = (v.cpu().numpy() for v in L._layer(x.view.double()[torch.from_numpy(some).cuda()], ids[some], None, win, wout, 1, inner))
+    assert np.all(np.abs(got[some] - want) <= err + 2.0 ** -24 * np.abs(want) * 1.001 + 2.0 ** -149)
