@@ -463,7 +463,7 @@ void layer_in(Layer p)
 // S > 1, for few columns: K falls into S parts, and the 16 rows of weights of a product are COLS columns in each of the parts, the 16 rows of h COLS rows in each of
 // them.  Of the product the S blocks of a part with itself are used; a wave reads as much as ever, and there are S times as many workgroups.
 // Of the same layers: 73 MB in 27 - 28 us, 8.8 MB in 6.7 - 7.5.
-constexpr int kShares = 1024;           // rows of 16 sums in the LDS
+constexpr int kShares = 1024;           // rows of 16 sums, or of the 32 of two tiles, in the LDS
 constexpr unsigned kNowhere = 0xf0000000u;      // behind the end of h, which has 3 * 2^30 bytes at most, with whatever is added to it
 
 template <typename T, typename Q, int W, int S, int NC, Ending ENDING>
