@@ -567,7 +567,7 @@ int opevo_matmul_mx4_grouped(const uint8_t *a, int64_t lda, const uint8_t *scale
  * with silu(g) = g / (1 + exp(-g)).  x and y [tokens][width] in dtype; expert and weight (fp32, or NULL: 1) [tokens * k] as opevo_route_dispatch and opevo_route_combine take them: a slot
  * whose id is outside [0, experts) adds nothing, whatever its weight, and a token without any other gets zeros.  w_in [experts][2 * inner][width]: the rows of Wg before those of Wu; w_out
  * [experts][width][inner]; all rows of either ld_* apart.  Weights in 8 bits with a scale for each row (scale_in [experts][2 * inner], scale_out [experts][width]), or in microscaled
- * 4 bits along their rows.  Activations are not quantised: x is taken as it is, h is kept to 2^-16 of its value (fp32 callers: as it is), sums are fp32, and y is rounded once.  tokens * k at
+ * 4 bits along their rows.  Activations are not quantised: x is taken as it is and h is kept in fp32 (of fp32 numbers below 2^-109 what lies under 2^-133 is cut off), sums are fp32, and y is rounded once.  tokens * k at
  * most OPEVO_EXPERT_LAYER_MAX_SLOTS (more: opevo_route_dispatch and the products by expert), width and inner at most 2^20. */
 #define OPEVO_EXPERT_LAYER_MAX_SLOTS 512
 /* Bytes of workspace (16-byte aligned) that a layer of this size takes.  Host only. */

@@ -3,8 +3,9 @@
 // weights in 8 bits with a scale a channel or in microscaled 4 bits (mx4.hpp), activations as they are.  What bounds it are the weights of the experts in use, each of which is read once; the
 // products go through bf16 matrix instructions because those hold 8-bit integers and E2M1 values under their factors exactly.
 //
-// Activations of more bits go as a sum of bf16 numbers, each in a row of the product of its own: fp16 is the sum of two, fp32 of three, exactly, and h, which is fp32, is kept as two (an error of
-// 2^-16; three for fp32 callers).  The product has 16 rows whatever they hold, so for the few rows of an expert the parts cost nothing, and the rows' sums are added at the end.
+// Activations of more bits go as a sum of bf16 numbers, each in a row of the product of its own: fp16 is the sum of two, fp32, and with it h, whatever the callers' type, of three: exactly, down to
+// magnitudes of 2^-109, whose last bit is bf16's smallest number 2^-133, below which what they hold is cut off.  The product has 16 rows whatever they hold, so for the few rows of an expert
+// the parts cost nothing, and the rows' sums are added at the end.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -151,8 +152,8 @@ struct Weights4 {
 
 // ------------------------------------------------------------------ activations
 // How many bf16 numbers make one of a type, and what a row that holds the part `part` gives to the product.
-template <typename T> struct Parts { static constexpr int n = 1, h = 2; };
-template <> struct Parts<_Float16> { static constexpr int n = 2, h = 2; };
+template <typename T> struct Parts { static constexpr int n = 1, h = 3; };
+template <> struct Parts<_Float16> { static constexpr int n = 2, h = 3; };
 template <> struct Parts<float> { static constexpr int n = 3, h = 3; };
 
 // Where value c of a row of h stands: the eight values that a lane takes of it at a time stand side by side with those that the lanes of the other three groups take at the same time, so that an
@@ -447,12 +448,10 @@ void layer_in(Layer p)
                 for (int o = 0; o < W; ++o) v[side] += ((const float *)&sums[o][side * NP + c / 16][c % 16 / 4 * 16 + at * PX + part])[c % 4];
         const float gate = v[0] * Q::scale(p.sin, first + c0 + c), up = v[1] * Q::scale(p.sin, first + p.inner + c0 + c);
         const float h = gate / (1.f + expf(-gate)) * up, second = rest(h);
+        static_assert(PH == 3, "");
         to[0] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(h) >> 16));
-        if constexpr (PH == 2) to[p.ld_h] = (__bf16)second;
-        else {
-            to[p.ld_h] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(second) >> 16));
-            to[2 * p.ld_h] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(rest(second)) >> 16));
-        }
+        to[p.ld_h] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(second) >> 16));
+        to[2 * p.ld_h] = __builtin_bit_cast(__bf16, (unsigned short)(__float_as_uint(rest(second)) >> 16));
     }
 }
 
@@ -625,7 +624,7 @@ int check_layer(const char *who, int64_t tokens, int k, int experts, int dtype, 
 }
 
 int64_t row_of_h(int64_t inner) { return (inner + 2 * kStep - 1) / (2 * kStep) * (2 * kStep); }
-size_t layer_workspace(int64_t slots, int dtype, int64_t inner) { return sizeof(Plan) + (size_t)slots * (dtype == OPEVO_F32 ? 3 : 2) * row_of_h(inner) * sizeof(__bf16); }
+size_t layer_workspace(int64_t slots, int64_t inner) { return sizeof(Plan) + (size_t)slots * Parts<float>::h * row_of_h(inner) * sizeof(__bf16); }
 
 template <typename T, typename Q>
 int run_layer(Layer p, hipStream_t stream)
@@ -633,10 +632,12 @@ int run_layer(Layer p, hipStream_t stream)
     constexpr int LONG = Q::SUB * kStep, PER = 16 / Parts<T>::n;
     const auto ending = [](int k) { return k % LONG == 0 ? kEven : k < (Q::SUB == 1 ? 16 : 31) ? kTiny : kRagged; };
     const Ending in = ending(p.width), of = ending(p.inner);
-    // The second launch: a workgroup to 16 columns for each compute unit, or parts of K as long as that leaves units without one (us, S = 1 / 2 / 4: 1024 columns, 1 token x 2 of 4096 inner ones in
-    // 8 bits 9.3 / 7.1 / 6.4; 2048 columns, 4 x 4 of 2048 30 / 20 / 22, 64 x 8 of 1024 118 / 100 / 187; 4096 columns, 1 x 8 of 1024 12.4 / 13.2 / 19) ...
-    const int tiles = (p.width + 15) / 16;
-    int parts = tiles <= 80 ? 4 : tiles <= 160 ? 2 : 1;
+    // The second launch: a workgroup to 16 columns for each compute unit, or parts of K as long as that leaves units without one and the slots are few: parts leave room for fewer rows of an expert in a
+    // product, whose weights are then read once more for the others (us, whole layers, S = 1 / 2 / 4: 1024 columns of 4096 inner ones, 1 token x 8 of 64 experts in 8 bits 48 / 39 / 34, 16 x 2 of 8 in
+    // 4 bits 36 / 37 / 51, 100 x 2 of 8 in 8 bits 100 / 154 / 265; 256 of 1024, 4 x 4 of 32 in fp32 17 / 15 / 15, 32 x 4 of 64 in 4 bits 25 / 26 / 29; 2048 of 1024, 1 x 8 of 64 22 / 20 / 21, 100 x 2 of
+    // 8 52 / 85 / 139) ...
+    const int tiles = (p.width + 15) / 16, work = p.slots * tiles;
+    int parts = tiles <= 80 ? (work < 1024 ? 4 : work <= 4096 ? 2 : 1) : tiles <= 160 && work < 1024 ? 2 : 1;
     while (parts > 1 && (p.inner % (parts * LONG) != 0 || 16 / parts < Parts<T>::h)) parts /= 2;
     // for many slots 32 columns a workgroup, which halve what it reads of h for its weights (4 bits, 32 tokens x 4 of 64 experts, 4096 x 1024, second launch, 28 us instead of 32; 63 x 5 of 72,
     // 2983 x 640 in fp16 101 in all instead of 122; 5 x 6 of 9, 2048 x 1868 45 instead of 36)
@@ -669,7 +670,7 @@ int plan_layer(const char *who, Layer *p, int dtype, int64_t tokens, int k, int 
     if (int rc = check_rows(who, "y", p->y, p->ld_y, width, size)) return rc;
     if (int rc = check_words(who, "expert", p->expert)) return rc;
     if (!aligned(p->weight, 4)) return fail(OPEVO_E_ARG, "%s: weight is not aligned to 4 bytes", who);
-    const size_t need = layer_workspace(tokens * k, dtype, inner);
+    const size_t need = layer_workspace(tokens * k, inner);
     if (!workspace || !aligned(workspace, 16) || bytes < need)
         return fail(OPEVO_E_ARG, "%s: the workspace holds %zu bytes of the %zu it takes, or is not aligned to 16 bytes", who, workspace ? bytes : 0, need);
     p->tokens = (int)tokens; p->k = k; p->slots = (int)tokens * k; p->experts = experts; p->width = (int)width; p->inner = (int)inner;
@@ -686,7 +687,7 @@ extern "C" int opevo_expert_layer_workspace(int64_t tokens, int k, int dtype, in
     const char *who = "expert_layer_workspace";
     if (!bytes) return fail(OPEVO_E_ARG, "%s: bytes is NULL", who);
     if (int rc = check_layer(who, tokens, k, 1, dtype, 1, inner)) return rc;
-    *bytes = tokens == 0 ? 0 : layer_workspace(tokens * k, dtype, inner);
+    *bytes = tokens == 0 ? 0 : layer_workspace(tokens * k, inner);
     return OPEVO_OK;
 }
 
