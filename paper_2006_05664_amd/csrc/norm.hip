@@ -433,7 +433,7 @@ int run_norm(Norm p, hipStream_t stream)
     auto *k = p.width % n == 0 ? (l.hold == 1 ? norm_rows<T, 1, TO8, kWhole> : l.hold == 2 ? norm_rows<T, 2, TO8, kWhole> : norm_rows<T, 4, TO8, kWhole>)
               : p.width > n && held ? (l.hold == 1 ? norm_rows<T, 1, TO8, kOverlap> : l.hold == 2 ? norm_rows<T, 2, TO8, kOverlap> : norm_rows<T, 4, TO8, kOverlap>)
                                     : norm_rows<T, 1, TO8, kRest>;
-    return launch("norm_rows launch", k, spread((p.rows + ty - 1) / ty), dim3(threads), stream, p);
+    return launch("norm_rows launch", k, spread((p.rows + ty - 1) / ty, 1, threads), dim3(threads), stream, p);
 }
 template <typename T> int run_plain(const Norm &p, hipStream_t stream) { return run_norm<T, false>(p, stream); }
 template <typename T> int run_to8(const Norm &p, hipStream_t stream) { return run_norm<T, true>(p, stream); }

@@ -10,12 +10,12 @@
 
 namespace {
 
-// A launch has fewer than 2^32 threads along an extent of its grid: workgroups go on in the third.
-constexpr int kGridX = 1 << 23;
-__device__ __forceinline__ long this_block() { return (long)blockIdx.z * kGridX + blockIdx.x; }
-inline dim3 spread(int64_t blocks, int64_t parts = 1)
+// A launch has fewer than 2^32 threads along an extent of its grid: workgroups go on in the third after as many as make 2^31.
+__device__ __forceinline__ long this_block() { return (long)blockIdx.z * gridDim.x + blockIdx.x; }
+inline dim3 spread(int64_t blocks, int64_t parts = 1, int threads = 256)
 {
-    return dim3((unsigned)std::min<int64_t>(blocks, kGridX), (unsigned)parts, (unsigned)((blocks + kGridX - 1) / kGridX));
+    const int64_t most = ((int64_t)1 << 31) / threads;
+    return dim3((unsigned)std::min(blocks, most), (unsigned)parts, (unsigned)((blocks + most - 1) / most));
 }
 
 // 16 bytes of a row.

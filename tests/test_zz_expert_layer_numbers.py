@@ -11,7 +11,6 @@ import test_zz_expert_layer as L
 from test_zz_experts import CODE, TINY, U, V, Matrix, _activations, _torch, _words, gpu
 from test_zz_mx4 import VALUES, Bytes, _pack
 
-
 class Rows:
     """Rows of small whole numbers as weights of either kind, as they are."""
 
@@ -28,7 +27,6 @@ class Rows:
             self.q = Bytes(rows, (K + 1) // 2, values=_pack(code.astype(np.uint8)))
             self.f = Bytes(rows, -(-K // 32), values=np.full((rows, -(-K // 32)), 127, dtype=np.uint8))
             self.args = (self.q.ptr, self.q.ld, self.f.ptr, self.f.ld)
-
 
 # tokens, k, experts, width, inner: each way of the second launch; rows of one expert in one unit and in several
 @gpu
