@@ -306,7 +306,7 @@ void norm_grad(Grad p)
             dot = of_waves(red[turn], tx, plus);
         }
         if (!on) return;
-        const float inv = now.inv, back = inv * inv * (dot / (float)p.width);
+        const float inv = now.inv, back = inv * (inv * (dot / (float)p.width));         // inv^2 alone may be beyond fp32, or too small for its 24 bits
         auto write = [&](int i, const Vec<T> &gi, const Vec<T> &si, const Vec<T> &wi, const Vec<T> &ai) {
             Vec<T> out;
 #pragma unroll

@@ -1,0 +1,30 @@
+"""Norms of rows at the ends of their numbers' range, where a step on the way leaves fp32 and the result does not.  Tolerances are those of the norms' other tests."""
+import numpy as np
+import pytest
+
+import paper_2006_05664_amd as P
+import test_zz_norms as N
+from test_zz_experts import CODE, U, V, Matrix, _activations, _torch, _words, gpu
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [2e-20, 1e-12, 1e15, 8e18])
+@pytest.mark.parametrize("width", [7, 300, 4099, 20011])
+def test_gradients_of_small_and_large_rows(width, size, dtype):
+    """eps = 0 and 1 / rms up to 5e19 or down to 1e-19, whose square fp32 does not hold, or not in 24 bits.  The gradient is about dy / rms."""
+    rng = np.random.default_rng(width)
+    rows = 9
+    sv = N._narrow(_activations(rng, rows, width, dtype) * np.float32(size), dtype)
+    gv, wv = _activations(rng, rows, width, dtype), N._weights(rng, width, dtype)
+    iv = N._inv(sv, 0.0).astype(np.float32)
+    assert np.isfinite(iv).all()
+    s, g, dx = Matrix(rows, width, dtype, values=sv), Matrix(rows, width, dtype, values=gv), Matrix(rows, width, dtype)
+    w, inv, dw = Matrix(1, width, dtype, values=wv[None]), _words(iv[:, 0], np.float32), _words(np.zeros(width), np.float32)
+    torch, _ = _torch()
+    bytes_ = P.opevo_norm_rows_grad_workspace(rows, width)
+    ws = torch.empty(max(bytes_, 4), dtype=torch.uint8, device="cuda")
+    P.opevo_norm_rows_grad(g.ptr, width, 0, 0, s.ptr, width, w.ptr, inv.data_ptr(), CODE[dtype], rows, width, dx.ptr, width, dw.data_ptr(), ws.data_ptr(), bytes_)
+    want, bound, want_w, bound_w = N._gradients(sv, wv, gv, None, iv)
+    assert np.all(np.abs(dx.host() - want) <= (N._terms(width) + 12) * U * bound * (1 + 1e-3) + V[dtype] * (1 + 1e-3) * np.abs(want))
+    assert np.all(np.abs(dw.cpu().numpy() - want_w) <= (rows + 4) * U * bound_w)
