@@ -74,13 +74,15 @@ template <> struct Exact<float> { typedef double type; };
 // q = round(127 v / a).  v times 127 / a in fp32 is off by at most three roundings, 127 * 3 * 2^-24 = 2.3e-5, and rounds to the same integer unless it is within 4e-5 of
 // the middle between two; then the quotients of the piece are formed in fp64, where the middle is hit only by quotients that are there.
 template <typename V> struct RowTo8 {
-    V a;
-    float inv, pre;
+    V a, pre;
+    float inv;
     bool on;
     __device__ explicit RowTo8(V a_) : a(a_)
     {
-        pre = a > (V)1e30 ? 0x1p-96f : a < (V)1e-30 ? 0x1p96f : 1.f;        // neither the factor nor its product overflows
-        inv = 127.f / (float)(a * (V)pre);
+        pre = a > (V)1e30 ? (V)0x1p-96 : a < (V)1e-30 ? (V)0x1p96 : (V)1;   // neither the factor nor its product overflows
+        if constexpr (sizeof(V) == 8)
+            if (a < 1e-60) pre = 0x1p192;           // products of two fp32 go down to 2^-298
+        inv = 127.f / (float)(a * pre);
         on = a > 0 && a <= (V)FLT_MAX;
     }
     template <int N> __device__ __forceinline__ void operator()(const V (&v)[N], int8_t (&q)[N]) const
@@ -89,7 +91,7 @@ template <typename V> struct RowTo8 {
         float off = 0.f;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float f = (float)(v[e] * (V)pre), r = fmaf(f, inv, kRound);
+            const float f = (float)(v[e] * pre), r = fmaf(f, inv, kRound);
             off = fmaxf(off, fabsf(fmaf(f, inv, kRound - r)));
             q[e] = (int8_t)(on ? (int)(__float_as_uint(r) & 0xff) : 0);
         }

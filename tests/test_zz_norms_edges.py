@@ -28,3 +28,38 @@ def test_gradients_of_small_and_large_rows(width, size, dtype):
     want, bound, want_w, bound_w = N._gradients(sv, wv, gv, None, iv)
     assert np.all(np.abs(dx.host() - want) <= (N._terms(width) + 12) * U * bound * (1 + 1e-3) + V[dtype] * (1 + 1e-3) * np.abs(want))
     assert np.all(np.abs(dw.cpu().numpy() - want_w) <= (rows + 4) * U * bound_w)
+
+
+def _in_8_bits(xv, wv, dtype, eps, rv=None, in_place=False):
+    rows, width = xv.shape
+    x, q = Matrix(rows, width, dtype, values=xv), Matrix(rows, width, "i8")
+    r = Matrix(rows, width, dtype, values=rv) if rv is not None else None
+    s = x if in_place else Matrix(rows, width, dtype)
+    w, scale = Matrix(1, width, dtype, values=wv[None]), _words(np.full(rows + 1, -7), np.float32)
+    P.opevo_norm_rows_i8(x.ptr, width, r.ptr if r else 0, width if r else 0, w.ptr, eps, CODE[dtype], rows, width, s.ptr, width, q.ptr, width, scale.data_ptr())
+    got, scales = q.host(), scale.cpu().numpy()
+    assert scales[-1] == -7
+    assert np.array_equal(s.host(), N._sum(xv, rv, dtype))
+    return got, scales[:-1]
+
+
+def _check_q(q, s, w):
+    v = s.astype(np.float64) * w.astype(np.float64)
+    a = np.abs(v).max(axis=1, keepdims=True)
+    exact = 127.0 * v / np.where(a > 0, a, 1.0)
+    near = np.abs(np.abs(exact - np.floor(exact)) - 0.5) <= 127 * 4 * 2.0 ** -53
+    assert not ((q != np.rint(exact)) & ~near).any()
+    return a[:, 0]
+
+
+@gpu
+@pytest.mark.parametrize("width", [3, 130, 700, 1500, 4096, 5001, 20011])
+def test_rows_in_8_bits_whose_factor_leaves_fp32(width):
+    """fp32 rows and weights whose product is 1e-68 and less, down to the product of two subnormal numbers: q as ever.  (The scale is below fp32: 0.)"""
+    rng = np.random.default_rng(width)
+    sizes = np.array([1e-31, 1e-35, 1e-38, 1e-42, 1.0, 0.0], dtype=np.float32)
+    wv = (1 + rng.random(width)).astype(np.float32) * np.float32(1e-37)
+    xv = ((1 + rng.random((len(sizes), width))) * np.where(rng.random((len(sizes), width)) < 0.5, -1, 1) * sizes[:, None]).astype(np.float32)
+    q, scale = _in_8_bits(xv, wv, "f32", N.EPS)
+    _check_q(q, xv, wv)
+    assert not scale[[0, 1, 2, 3, 5]].any() and np.isfinite(scale).all()
