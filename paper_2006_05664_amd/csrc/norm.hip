@@ -223,7 +223,8 @@ void norm_rows(Norm p)
         if (lane + u * tx < count) write(lane + u * tx, s[u], by[u]);
     if (WAY != kOverlap)
         for (int i = lane + HOLD * tx; i < count; i += tx) write(i, again(i), weights(i));
-    if (lane == 0 && p.per_row) p.per_row[row] = !TO8 ? inv : most <= (V)FLT_MAX ? (float)(most * (V)inv / (V)127) : __uint_as_float(0x7fc00000u);
+    // in fp64: a i may be beyond fp32 and its 127th part not
+    if (lane == 0 && p.per_row) p.per_row[row] = !TO8 ? inv : most <= (V)FLT_MAX ? (float)((double)most * (double)inv / 127.0) : __uint_as_float(0x7fc00000u);
 }
 
 // ------------------------------------------------------------------ gradient

@@ -63,3 +63,17 @@ def test_rows_in_8_bits_whose_factor_leaves_fp32(width):
     q, scale = _in_8_bits(xv, wv, "f32", N.EPS)
     _check_q(q, xv, wv)
     assert not scale[[0, 1, 2, 3, 5]].any() and np.isfinite(scale).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_scale_that_fp32_holds_and_its_127_fold_not(dtype):
+    """One number among 4096: i = 64, so that a i = 64 * 3e38 is beyond fp32 and scale = a i / 127 is not."""
+    rng = np.random.default_rng(1)
+    rows, width = 3, 4096
+    xv, wv = np.zeros((rows, width), dtype=np.float32), N._narrow(np.full(width, 3e38), dtype)
+    xv[np.arange(rows), rng.integers(0, width, rows)] = [1.0, -0.5, 1.0]
+    q, scale = _in_8_bits(xv, wv, dtype, 0.0)
+    a = _check_q(q, xv, wv)
+    want = a * N._inv(xv, 0.0)[:, 0] / 127.0
+    assert np.all(np.abs(scale - want) <= (N._i_err(width) + 3 * U) * want)
