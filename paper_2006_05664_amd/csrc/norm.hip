@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cstdint>
+#include <type_traits>
 
 #include "launch.hpp"
 #include "narrow.hpp"
@@ -67,9 +68,11 @@ template <typename V, typename F> __device__ __forceinline__ V of_waves(const V 
     return v;
 }
 
-// s w as the quantiser takes it: without rounding.  The product of two bf16 has 16 bits and that of two fp16 22, so fp32 holds it; fp32's takes 48 and goes into fp64.
+// s w as the quantiser takes it: without rounding.  The product of two bf16 has 16 bits and that of two fp16 22, so fp32 holds it; fp32's takes 48 and goes into fp64.  Products of two bf16 below 2^-126 lose
+// bits in fp32, but what is less than a 256th of the row's largest is 0 in 8 bits: rows whose largest is below kTiny, and they alone, are taken once more, in fp64.
 template <typename T> struct Exact { typedef float type; };
 template <> struct Exact<float> { typedef double type; };
+constexpr float kTiny = 0x1p-110f;
 
 // q = round(127 v / a).  v times 127 / a in fp32 is off by at most three roundings, 127 * 3 * 2^-24 = 2.3e-5, and rounds to the same integer unless it is within 4e-5 of
 // the middle between two; then the quotients of the piece are formed in fp64, where the middle is hit only by quotients that are there.
@@ -199,7 +202,8 @@ void norm_rows(Norm p)
         if (TO8) most = of_waves(red8, tx, larger);
     }
     const float inv = 1.f / sqrtf(squares / (float)p.width + p.eps);
-    if (!on) return;
+    constexpr bool TWICE = TO8 && std::is_same<T, __bf16>::value;      // rows may be taken once more, by waves that meet
+    if (!TWICE && !on) return;          // (8192 rows of 4096 fp32 in 8 bits 69 us, 73 without)
     const RowTo8<V> to8(most);
     T *sum = (T *)p.sum + row * p.ld_sum;
     auto write = [&](int i, const Vec<T> &v, const Vec<T> &by) {
@@ -223,8 +227,47 @@ void norm_rows(Norm p)
         if (lane + u * tx < count) write(lane + u * tx, s[u], by[u]);
     if (WAY != kOverlap)
         for (int i = lane + HOLD * tx; i < count; i += tx) write(i, again(i), weights(i));
-    // in fp64: a i may be beyond fp32 and its 127th part not
-    if (lane == 0 && p.per_row) p.per_row[row] = !TO8 ? inv : most <= (V)FLT_MAX ? (float)((double)most * (double)inv / 127.0) : __uint_as_float(0x7fc00000u);
+    const auto scale = [&](auto most) { return most <= FLT_MAX ? (float)((double)most * (double)inv / 127.0) : __uint_as_float(0x7fc00000u); };      // in fp64: a i may be beyond fp32 and its 127th part not
+    if (on && lane == 0 && p.per_row) p.per_row[row] = TO8 ? scale(most) : inv;
+    if constexpr (TWICE) {
+        // Behind what all rows take, where it costs them least (16384 rows of 4096: 97 us without, 100 like this, 101 - 103 with it in front); s stands in memory by now, and a lane reads what it
+        // has written.
+        bool tiny = on && most < kTiny;
+        if (tx == 128) {                    // alike for the whole workgroup, whose waves meet: two rows
+            const int other = ((int)threadIdx.x >> 6 & ~1) ^ 2;
+            tiny |= (row ^ 1) < p.rows && fmaxf(red8[other], red8[other + 1]) < kTiny;
+        }
+        if (__ballot(tiny) == 0) return;
+        __shared__ double red64[kMostLanes / 64];
+        const T *from = p.sum ? sum : x;
+        double largest = 0;
+        auto each = [&](auto &&f) {
+#pragma unroll 1
+            for (int i = lane; i < count; i += tx)
+#pragma unroll 1
+                for (int c = at.first(i); c < min(at.first(i) + n, p.width); ++c) {
+                    T s;
+                    __builtin_memcpy(&s, from + c, sizeof s);           // may be what was stored there as another type
+                    f(c, w ? (double)s * (double)w[c] : (double)s);
+                }
+        };
+        each([&](int, double v) { largest = fmax(largest, fabs(v) <= (double)FLT_MAX ? fabs(v) : (double)INFINITY); });
+        const auto larger64 = [](double a, double b) { return fmax(a, b); };
+        largest = of_wave(largest, tx, larger64);
+        if (tx > 64) {
+            if ((threadIdx.x & 63) == 0) red64[threadIdx.x >> 6] = largest;
+            __syncthreads();
+            largest = of_waves(red64, tx, larger64);
+        }
+        const RowTo8<double> again8(largest);
+        each([&](int c, double v) {
+            const double one[1] = {v};
+            int8_t q[1];
+            again8(one, q);
+            ((int8_t *)p.y)[row * p.ld_y + c] = q[0];
+        });
+        if (on && lane == 0) p.per_row[row] = scale(largest);
+    }
 }
 
 // ------------------------------------------------------------------ gradient

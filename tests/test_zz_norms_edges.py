@@ -77,3 +77,27 @@ def test_a_scale_that_fp32_holds_and_its_127_fold_not(dtype):
     a = _check_q(q, xv, wv)
     want = a * N._inv(xv, 0.0)[:, 0] / 127.0
     assert np.all(np.abs(scale - want) <= (N._i_err(width) + 3 * U) * want)
+
+
+# a row of every way a workgroup holds rows in: in one wave, in two of its four, in the whole of it; held and not
+@gpu
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("rows,width", [(1, 3), (40, 130), (41, 700), (9, 1500), (8, 4096), (5, 5001), (7, 20011), (3, 8192)])
+def test_rows_in_8_bits_whose_products_fp32_does_not_hold(rows, width, residual):
+    """bf16 rows of 1e-18 under weights of 1e-22 to 1e-36, with eps = 0: the products are below fp32, where they lose bits and then all of them, and what they make of the row is not.  Rows of other sizes,
+    and of zeros, stand between them."""
+    rng = np.random.default_rng(width)
+    for size in (1e-22, 1e-25, 1e-30, 1e-36):
+        wv = N._narrow((1 + rng.random(width)) * size, "bf16")
+        xv = _activations(rng, rows, width, "bf16") + 0.1
+        xv = N._narrow(xv * np.array([1e-18, 1e-17, 1.0, 1e12])[np.arange(rows) % 4][:, None], "bf16")
+        rv = N._narrow(0.3 * rng.standard_normal((rows, width)) * 1e-18, "bf16") if residual else None
+        xv[rows // 2] = 0 if rows > 1 else xv[rows // 2]
+        if residual:
+            rv[rows // 2] = 0
+        s = N._sum(xv, rv, "bf16")
+        q, scale = _in_8_bits(xv, wv, "bf16", 0.0, rv, in_place=residual)
+        a = _check_q(q, s, wv)
+        on = a > 0
+        want = a[on] * N._inv(s[on], 0.0)[:, 0] / 127.0
+        assert np.all(np.abs(scale[on] - want) <= (N._i_err(width) + 3 * U) * want + 2.0 ** -150)
