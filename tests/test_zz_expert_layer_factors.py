@@ -5,7 +5,8 @@ import pytest
 
 import paper_2006_05664_amd as P
 import test_zz_expert_layer as L
-from test_zz_experts import CODE, V, Matrix, _activations, _torch, _words, gpu
+from test_zz_expert_layer_numbers import Rows
+from test_zz_experts import CODE, U, V, Matrix, _activations, _torch, _words, gpu
 from test_zz_mx4 import VALUES
 
 
@@ -101,3 +102,34 @@ def test_small_activations(dtype, kind):
     L._layer.dtype = dtype
     want, err = (v.cpu().numpy() for v in L._layer(x.view.double(), ids, None, win, wout, experts, inner))
     assert np.all(np.abs(y.host() - want) <= err + V[dtype] * (1 + 1e-3) * np.abs(want))
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["i8", "mx4"])
+@pytest.mark.parametrize("exponent", [-100, -109])
+def test_the_last_bit_of_a_small_activation(kind, exponent):
+    """One number of x counts, and its gate and up are 2^-exponent of it: y = silu(g) g with g in [1, 2), whose roundings (the sum of x's three parts 2u and the factor u for either, twice that through silu's slope of
+    at most 2 g sigmoid(g) relative to itself; exp, quotient and products 8u; the sum of h's three parts 2u and the output u) make less than 24 u; without the last of the three parts, 2^-16 of x, it would be 256 u and more."""
+    torch, _ = _torch()
+    rng = np.random.default_rng(-exponent)
+    tokens, width, inner = 64, 256, 128
+    xv = np.zeros((tokens, width), dtype=np.float32)
+    g = 1 + rng.random(tokens).astype(np.float32).astype(np.float64)
+    g = g.astype(np.float32)
+    xv[:, 0] = g * np.float32(2.0 ** exponent)
+    assert np.array_equal(xv[:, 0].astype(np.float64) * 2.0 ** -exponent, g.astype(np.float64))
+    ones_in, ones_out = np.zeros((2 * inner, width)), np.zeros((width, inner))
+    ones_in[:, 0] = 1
+    ones_out[:, 5] = 1
+    win, wout = Rows(ones_in, kind), Rows(ones_out, kind)
+    if kind == "i8":
+        win.scale *= 2.0 ** -exponent
+    else:
+        win.f.view += -exponent
+    x, y = Matrix(tokens, width, "f32", values=xv), Matrix(tokens, width, "f32")
+    size = P.opevo_expert_layer_workspace(tokens, 1, CODE["f32"], inner)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    L._call(kind, x, "f32", _words(np.zeros((tokens, 1)), np.int32), None, tokens, 1, 1, width, inner, win, wout, y, ws, size)
+    g = g.astype(np.float64)
+    want = (g / (1 + np.exp(-g)) * g)[:, None]
+    assert np.all(np.abs(y.host() - want) <= 24 * U * want), (np.abs(y.host() / want - 1) / U).max()
