@@ -461,7 +461,7 @@ void layer_in(Layer p)
 // they belong to: an iteration is a few microseconds' worth of latency and a fraction of one of work.
 // S > 1, for few columns: K falls into S parts, and the 16 rows of weights of a product are COLS columns in each of the parts, the 16 rows of h COLS rows in each of
 // them.  Of the product the S blocks of a part with itself are used; a wave reads as much as ever, and there are S times as many workgroups.
-// Of the same layers: 73 MB in 27 - 28 us, 8.8 MB in 6.7 - 7.5.
+// Of the same layers: 82 MB in 31 - 32 us, 9 MB in 7.8 - 8.2.
 constexpr int kShares = 1024;           // rows of 16 sums, or of the 32 of two tiles, in the LDS
 constexpr unsigned kNowhere = 0xf0000000u;      // behind the end of h, which has 3 * 2^30 bytes at most, with whatever is added to it
 
@@ -639,14 +639,14 @@ int run_layer(Layer p, hipStream_t stream)
     const int tiles = (p.width + 15) / 16, work = p.slots * tiles;
     int parts = tiles <= 80 ? (work < 1024 ? 4 : work <= 4096 ? 2 : 1) : tiles <= 160 && work < 1024 ? 2 : 1;
     while (parts > 1 && (p.inner % (parts * LONG) != 0 || 16 / parts < Parts<T>::h)) parts /= 2;
-    // for many slots 32 columns a workgroup, which halve what it reads of h for its weights (4 bits, 32 tokens x 4 of 64 experts, 4096 x 1024, second launch, 28 us instead of 32; 63 x 5 of 72,
-    // 2983 x 640 in fp16 101 in all instead of 122; 5 x 6 of 9, 2048 x 1868 45 instead of 36)
+    // for many slots 32 columns a workgroup, which halve what it reads of h for its weights (us, whole layers, 32 columns / 16: 32 tokens x 4 of 64 experts, 4096 x 1024 in 4 bits 105 / 108; 63 x 5 of 72,
+    // 2983 x 640 in fp16 135 / 156; 64 x 8 of 64, 4096 x 1024 in 8 bits 235 / 291; 5 x 6 of 9, 2048 x 1868 44 / 36)
     const bool wide = parts == 1 && p.slots >= 80 && p.width >= 1024;
     auto *out = wide ? (of == kTiny ? layer_out<T, Q, 8, 1, 2, kTiny> : of == kRagged ? layer_out<T, Q, 8, 1, 2, kRagged> : layer_out<T, Q, 8, 1, 2, kEven>)
                 : of == kTiny ? layer_out<T, Q, 8, 1, 1, kTiny> : of == kRagged ? layer_out<T, Q, 8, 1, 1, kRagged>
                 : parts == 4 ? layer_out<T, Q, 8, 4, 1, kEven> : parts == 2 ? layer_out<T, Q, 8, 2, 1, kEven> : layer_out<T, Q, 8, 1, 1, kEven>;
-    // ... and where that is not enough the tokens in groups, each of which reads its experts' weights again, mostly from the caches (us, one sequence of iterations and groups against neither: 4-bit
-    // weights, 102 tokens x 2 of 8 experts, 246 columns of 2879 inner ones, fp16 61 / 132; 126 x 1 of 15, 469 of 1280, fp32 47 / 81; 8 bits, 32 x 1 of 62, 64 of 525 10 / 19)
+    // ... and where that is not enough the tokens in groups, each of which reads its experts' weights again, mostly from the caches (us, groups / one: 4-bit weights, 102 tokens x 2 of 8 experts, 246
+    // columns of 2879 inner ones, fp16 57 / 169; 126 x 1 of 15, 469 of 1280, fp32 50 / 82; 8 bits, 32 x 1 of 62, 64 of 525 11 / 27)
     const int cols = wide ? 32 : 16 / parts, across = (p.width + cols - 1) / cols;
     p.groups = std::min(p.tokens, std::max(1, 256 / across));
     p.group_tokens = (p.tokens + p.groups - 1) / p.groups;

@@ -486,7 +486,9 @@ void product4_tile(Product4 p)
 // ------------------------------------------------------------------ tiles of long rows
 // The same for operands that can come straight to LDS and whose K is a multiple of 1024, so that nothing is ragged.  The factors come for four slabs at a time, 32 bytes a row, two sets in turn:
 // eight bytes a row with every slab take as many requests as the codes, and cost 8192^3 some 40 us.  A set stands as two halves of [rows][16] bytes, each for two slabs.
-// 8192^3, 256 x 256: 238 - 250 us (4.4 - 4.6 PFLOP/s), matrix pipes 58 % busy, 196 on zeros: what is between is power.  The instruction alone, from registers, makes 6.7 PFLOP/s of random codes.
+// 8192^3, 256 x 256: 238 - 250 us (4.4 - 4.6 PFLOP/s), matrix pipes 59 % busy.  The instruction alone, from registers, makes 6.7 PFLOP/s of random codes and 9.4 of zeros; on zeros the kernel takes
+// 196 - 206 us where that would be 117: power is a part of what it lacks, waits for LDS and barriers (34 % of the waves' time) the other.
+// Factors start on multiples of 4 bytes: 16-byte loads take those.
 template <int BM_, int BN_, int WM_, int WN_, int STAGES_>
 struct LongShape {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, BK = 128, ROWS = BM + BN;

@@ -1,6 +1,7 @@
 // Rows of numbers to microscaled 4 bits (mx4.hpp) and back.  Of every 32 values the largest magnitude's exponent less 2 becomes the factor's, so that it lands in [4, 8); a value over
 // the factor is rounded to the nearest E2M1, ties to the even code, 6 at most.  The hardware's conversions round like that.  Bound by memory: a value is read once and
-// half a byte written (8192 rows of 4096 in bf16 22.5 us, 3.7 TB/s; back 14 us, the codes still in the caches).
+// half a byte written (8192 rows of 4096 in bf16 22.5 us, 3.7 TB/s, waves waiting 84 % of their time: a lane stores four bytes of codes, one in four a byte of
+// factors; back 14 us, the codes still in the caches).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

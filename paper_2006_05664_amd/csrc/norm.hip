@@ -117,7 +117,7 @@ struct Norm {
     float eps;
 };
 
-// 16384 rows of 4096 bf16 with a residual: 537 MB in 87 us (6.2 TB/s; a large copy takes 104 for as many bytes); in 8 bits 84.  32 rows: 3.2 us, a launch and a
+// 16384 rows of 4096 bf16 with a residual: 537 MB in 87 us (6.2 TB/s; a large copy takes 104 for as many bytes); in 8 bits 96, with more instructions a value than memory hides.  32 rows: 3.2 us, a launch and a
 // chain of latencies.  As many lanes as a row has pieces, up to 512: two pieces on 256 lanes and four on 128 take as long, eight on 64 half as long again.
 template <typename T, int HOLD, bool TO8, Way WAY>
 __global__ __launch_bounds__(kMostLanes)
@@ -282,7 +282,7 @@ struct Grad {
     int width, tx;
 };
 
-// Bound by memory: 8192 rows of 4096 bf16 with a gradient of the sum, 268 MB, in 47 - 52 us (5.2 - 5.7 TB/s) and 3 - 5 for the weight's partial sums.  A workgroup goes from row to row, the next one on its way,
+// Bound by memory: 8192 rows of 4096 bf16 with a gradient of the sum, 268 MB, in 51 - 54 us (5.0 - 5.3 TB/s) and 4 - 5 for the weight's partial sums.  A workgroup goes from row to row, the next one on its way,
 // with its share of the weight's gradient in registers; 512 workgroups (256: 66 us, 1024: 52).
 template <typename T, int HOLD, Way WAY>
 __global__ __launch_bounds__(kMostLanes)
